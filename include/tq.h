@@ -357,17 +357,122 @@ tq_status tq_decompress_aggregate_segments(const uint32_t* packed_dev, size_t wo
                                            const tq_params_t* params_dev, uint32_t num_levels,
                                            const float* weights_host, float* out_dev, void* stream);
 
+/*
+ * ---- Microscaled 4-bit floating point (MX) ------------------------------------------------------------------
+ *
+ * A second 4-bit family beside the codebooks above, for matrices that a training step multiplies and for messages.  A
+ * matrix [rows][cols] holds an E2M1 code for every element (magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6; bit 3 is the sign) and an
+ * E8M0 scale byte b, worth 2^(b - 127), for every 32 neighbours in a row; b = 255 stands for NaN.  The value of an
+ * element is magnitude * scale.
+ *   codes    row r starts at codes + r * code_stride; element c is the low (c even) or high nibble of byte c / 2.  A row
+ *            that ends inside a block of 32 is filled up with zero codes.
+ *   scales   TQ_MX_ROWS:  block c / 32 of row r is byte r * scale_stride + c / 32.
+ *            TQ_MX_TILES: tiles of 128 rows x 4 blocks, as the tensor cores take them.  With block b it is byte
+ *            (r / 128) * scale_stride + (b / 4) * 512 + (r % 32) * 16 + (r / 32 % 4) * 4 + b % 4.  The rest of the last tiles (rows
+ *            up to a multiple of 128, blocks up to a multiple of 4) must not be 255; the calls that write a matrix fill it with zeros.
+ *   codes and scales are device memory, 16-byte aligned; both strides are in bytes, multiples of 16 and at least
+ *   tq_mx_code_stride(cols) and tq_mx_scale_stride(cols, layout).  A scale buffer has `rows` rows (TQ_MX_ROWS) or ceil(rows / 128)
+ *   (TQ_MX_TILES).  Rows, and columns at multiples of 128, of a larger matrix make a matrix of their own (in TQ_MX_TILES rows from a multiple of 128).
+ * rows < 2^31; cols <= 2^40 (below 2^31 in the products).
+ */
+typedef enum { TQ_MX_TILES = 0, TQ_MX_ROWS = 1 } tq_mx_layout;
+typedef enum {
+    TQ_MX_NEAREST = 0,     /* scale 2^(floor(log2 max) - 2); to nearest, ties to the even code, magnitudes above 6 become 6 */
+    TQ_MX_STOCHASTIC = 1   /* the smallest power of two at which no element exceeds 6; E[value] = element, see tq_mx_quantize */
+} tq_mx_rounding;
+typedef enum {
+    TQ_MX_SILU = 0,        /* x / (1 + exp(-x)) */
+    TQ_MX_GELU = 1         /* x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
+} tq_mx_activation;
+typedef struct {
+    uint8_t* codes;
+    uint8_t* scales;
+    uint64_t rows, cols;
+    uint64_t code_stride, scale_stride;
+    uint32_t layout;       /* tq_mx_layout */
+    uint32_t reserved;
+} tq_mx_t;
+size_t tq_mx_code_stride(uint64_t cols);
+size_t tq_mx_scale_stride(uint64_t cols, tq_mx_layout layout);
+
+/*
+ * Quantisation of x [out->rows][out->cols] along its rows.
+ *   x_dev        elements of `dtype`, aligned to their size; x_stride >= cols elements from row to row.  Rows that start on 16-byte
+ *                boundaries are read fastest.
+ *   seed, first_row  stochastic rounding only.  Element (r, c) draws its 16 bits as in tq_compress: Philox4x32-10 with key = seed and
+ *                counter = (c >> 3, first_row + r, 0), slot c & 7.  With p the place between its two neighbours on the grid it goes
+ *                to the upper one when the bits are below rint(p * 2^16).
+ *   out_host     where the codes and scales go (the record is read during the call).
+ * A block with a NaN or an infinity gets zero codes and the scale 255, so that it decodes as NaN.  A block of zeros gets
+ * the scale byte 0.
+ * tq_mx_quantize_both also writes the transposed copy, out_t [cols][rows], whose blocks run along x's columns; the random bits
+ * are those of the element, the same in both.
+ * Errors: INVALID_ARG, ALIGNMENT, BUFFER_TOO_SMALL (a stride), CUDA.
+ */
+tq_status tq_mx_quantize(const void* x_dev, tq_dtype dtype, uint64_t x_stride, tq_mx_rounding rounding, uint64_t seed,
+                         uint32_t first_row, const tq_mx_t* out_host, void* stream);
+tq_status tq_mx_quantize_both(const void* x_dev, tq_dtype dtype, uint64_t x_stride, tq_mx_rounding rounding, uint64_t seed,
+                              uint32_t first_row, const tq_mx_t* out_host, const tq_mx_t* out_t_host, void* stream);
+
+/* The values of a matrix: out_dev [rows][cols] of `dtype`, aligned to its element size, out_stride >= cols elements from row to row.
+ * Exact, but for scales above 2^125 whose values pass the type's range and become infinite.  Errors as above. */
+tq_status tq_mx_dequantize(const tq_mx_t* m_host, void* out_dev, tq_dtype dtype, uint64_t out_stride, void* stream);
+
+/*
+ * Server side with MX rows as messages: row i of m (layout TQ_MX_ROWS, at most TQ_MAX_WORKERS rows) is worker i's gradient.
+ * out_j = sum_i w_i * value_ij, arithmetic, weights_host and out_dev [cols] as in tq_decompress_aggregate.
+ * Errors: INVALID_ARG, ALIGNMENT, BUFFER_TOO_SMALL, CUDA.
+ */
+tq_status tq_mx_decompress_aggregate(const tq_mx_t* m_host, const float* weights_host, float* out_dev, void* stream);
+
+/*
+ * out [a->rows][b->rows] = a b^T: both matrices [..][cols] with the same number of columns, layout TQ_MX_TILES.  Products of
+ * codes and scales are exact, sums are fp32 in the tensor cores' order (fixed for given sizes), each output is rounded once to `dtype`.
+ *   out_dev      aligned to its element size, out_stride >= b->rows elements from row to row.
+ * cols = 0 gives zeros.  Bounded waits as in tq_wait_expired_count.  Errors: INVALID_ARG, ALIGNMENT, BUFFER_TOO_SMALL, CUDA.
+ */
+tq_status tq_mx_product(const tq_mx_t* a_host, const tq_mx_t* b_host, void* out_dev, tq_dtype dtype, uint64_t out_stride,
+                        void* stream);
+
+/*
+ * The first half of a gated feed-forward block: with g = x w_gate^T and u = x w_up^T,
+ *     h = quantised (nearest, along the rows) act(g) * u.
+ * x [tokens][d], w_gate and w_up [features][d], h [tokens][features], all TQ_MX_TILES; features a multiple of 32, d >= 1.  g and u
+ * stay on the chip in fp32; h is made from them without an intermediate rounding.
+ *   projections_dev  NULL, or where the training step keeps [g | u] for tq_mx_gated_backward: [tokens][2 features] of `dtype`, proj_stride
+ *                    elements from row to row.
+ * Errors as for tq_mx_product.
+ */
+tq_status tq_mx_gated(const tq_mx_t* x_host, const tq_mx_t* w_gate_host, const tq_mx_t* w_up_host, tq_mx_activation activation,
+                      const tq_mx_t* h_host, void* projections_dev, tq_dtype dtype, uint64_t proj_stride, void* stream);
+
+/*
+ * Its backward pass up to the products: from dh [tokens][features] and the kept projections [g | u] (both of `dtype`),
+ *     dg = dh * u * act'(g),   du = dh * act(g),   h = act(g) * u      (fp32)
+ * are written as MX operands of the gradients' products:
+ *   dgu     [tokens][2 features]  [dg | du] along its rows:        d x = dgu (w_gate; w_up stacked, quantised along its columns)
+ *   dgu_t   [2 features][tokens]  its transposed copy:             d [w_gate; w_up] = dgu_t x_t
+ *   h_t     [features][tokens]    h along the tokens (nearest):    d w_down = dy_t h_t
+ * so that every one of them is a tq_mx_product.  `rounding` and `seed` apply to dgu and dgu_t, with the random bits of tq_mx_quantize_both on the
+ * matrix [dg | du] (first_row 0).  features is a multiple of 32.
+ * Errors as for tq_mx_quantize.
+ */
+tq_status tq_mx_gated_backward(const void* dh_dev, uint64_t dh_stride, const void* projections_dev, uint64_t proj_stride, tq_dtype dtype,
+                               tq_mx_activation activation, tq_mx_rounding rounding, uint64_t seed, const tq_mx_t* dgu_host,
+                               const tq_mx_t* dgu_t_host, const tq_mx_t* h_t_host, void* stream);
+
 const char* tq_strerror(tq_status status);
 int tq_last_cuda_error(void);   /* cudaError_t of the last failed runtime call on this thread, else 0 */
 uint64_t tq_kernel_launches(void); /* kernels launched by this library in this process so far */
 
-/* Bounded waits.  The large-input decompression kernel stages packed bytes through asynchronous bulk
+/* Bounded waits.  The large-input decompression kernel (and the products of MX matrices) stages packed bytes through asynchronous bulk
  * copies and waits for them on shared-memory barriers; every such wait gives up after a fixed number
  * of polls.  While barriers remain in the tile's loop the whole block takes the decision (it stores nothing for
  * the tile and counts itself once); in the last three steps of a tile there is no barrier left, and a thread whose
  * wait runs out there drops its own outputs and counts itself, so a tile can then be partly stored.
  * *count_host receives the number of such give-ups on the current device since the library was loaded
- * (0 in a healthy run: a non-zero value means the outputs of the affected launch are incomplete).
+ * (0 in a healthy run: a non-zero value means the outputs of the affected launch are incomplete).  A block of a product that gives up
+ * stops there, counts itself once and leaves the rest of its outputs unwritten.
  * Synchronises the device.  Returns TQ_ERR_INVALID_ARG for a null pointer, TQ_ERR_CUDA if the read fails.
  * (The paper has no counterpart; this is a health check of the implementation.) */
 tq_status tq_wait_expired_count(uint32_t* count_host);

@@ -25,12 +25,17 @@ _BITS = {2: 1, 4: 2, 8: 3, 16: 4}          # of a codebook with that many levels
 F32, BF16 = 0, 1
 UNIFORM, NONUNIFORM, BISCALED = 0, 1, 2
 ALPHA_CLOSED, ALPHA_FIXED_POINT, ALPHA_USER, ALPHA_MAXABS = 0, 1, 2, 3
+MX_TILES, MX_ROWS = 0, 1
+MX_NEAREST, MX_STOCHASTIC = 0, 1
+MX_SILU, MX_GELU = 0, 1
 FLAG_ALPHA_CAPPED, FLAG_ALPHA_AT_GMIN, FLAG_GAMMA_FROM_MLE, FLAG_INVALID = 1, 2, 4, 8
 
 EXPORTS = ("tq_packed_words", "tq_stats_workspace_bytes", "tq_stats", "tq_stats_hinted", "tq_stats_static", "tq_params", "tq_params_batch", "tq_params_from_levels", "tq_params_device",
            "tq_compress_device_params", "tq_decompress_aggregate_device_params",
            "tq_compress", "tq_decompress_aggregate", "tq_decompress_aggregate_rows", "tq_decompress_aggregate_apply",
-           "tq_segments_packed_words", "tq_stats_segments", "tq_stats_hinted_segments", "tq_compress_segments", "tq_decompress_aggregate_segments", "tq_strerror", "tq_last_cuda_error", "tq_kernel_launches", "tq_wait_expired_count")
+           "tq_segments_packed_words", "tq_stats_segments", "tq_stats_hinted_segments", "tq_compress_segments", "tq_decompress_aggregate_segments",
+           "tq_mx_code_stride", "tq_mx_scale_stride", "tq_mx_quantize", "tq_mx_quantize_both", "tq_mx_dequantize", "tq_mx_decompress_aggregate", "tq_mx_product",
+           "tq_mx_gated", "tq_mx_gated_backward", "tq_strerror", "tq_last_cuda_error", "tq_kernel_launches", "tq_wait_expired_count")
 
 
 class Stats(C.Structure):
@@ -49,6 +54,15 @@ class Params(C.Structure):
 
 
 assert C.sizeof(Stats) == 64 and C.sizeof(Params) == 176
+
+
+class Mx(C.Structure):
+    """tq_mx_t (56 bytes)."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("code_stride", C.c_uint64), ("scale_stride", C.c_uint64), ("layout", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+assert C.sizeof(Mx) == 56
 
 
 class TqError(RuntimeError):
@@ -110,6 +124,16 @@ def lib() -> C.CDLL:
         L.tq_compress_segments.restype = C.c_int
         L.tq_decompress_aggregate_segments.argtypes = [vp, sz, u32, C.POINTER(Segment), u32, vp, u32, C.POINTER(f32), vp, vp]
         L.tq_decompress_aggregate_segments.restype = C.c_int
+        mx = C.POINTER(Mx)
+        L.tq_mx_code_stride.argtypes = [u64]; L.tq_mx_code_stride.restype = sz
+        L.tq_mx_scale_stride.argtypes = [u64, C.c_int]; L.tq_mx_scale_stride.restype = sz
+        L.tq_mx_quantize.argtypes = [vp, C.c_int, u64, C.c_int, u64, u32, mx, vp]; L.tq_mx_quantize.restype = C.c_int
+        L.tq_mx_quantize_both.argtypes = [vp, C.c_int, u64, C.c_int, u64, u32, mx, mx, vp]; L.tq_mx_quantize_both.restype = C.c_int
+        L.tq_mx_dequantize.argtypes = [mx, vp, C.c_int, u64, vp]; L.tq_mx_dequantize.restype = C.c_int
+        L.tq_mx_decompress_aggregate.argtypes = [mx, C.POINTER(f32), vp, vp]; L.tq_mx_decompress_aggregate.restype = C.c_int
+        L.tq_mx_product.argtypes = [mx, mx, vp, C.c_int, u64, vp]; L.tq_mx_product.restype = C.c_int
+        L.tq_mx_gated.argtypes = [mx, mx, mx, C.c_int, mx, vp, C.c_int, u64, vp]; L.tq_mx_gated.restype = C.c_int
+        L.tq_mx_gated_backward.argtypes = [vp, u64, vp, u64, C.c_int, C.c_int, C.c_int, u64, mx, mx, mx, vp]; L.tq_mx_gated_backward.restype = C.c_int
         L.tq_strerror.argtypes = [C.c_int]; L.tq_strerror.restype = C.c_char_p
         L.tq_last_cuda_error.restype = C.c_int
         L.tq_kernel_launches.restype = u64
@@ -122,7 +146,8 @@ def lib() -> C.CDLL:
 _NATIVE = ("tq_stats", "tq_stats_hinted", "tq_stats_static", "tq_params_batch", "tq_params_device", "tq_compress", "tq_compress_device_params",
            "tq_decompress_aggregate", "tq_decompress_aggregate_rows", "tq_decompress_aggregate_apply",
            "tq_decompress_aggregate_device_params", "tq_stats_segments", "tq_stats_hinted_segments", "tq_compress_segments",
-           "tq_decompress_aggregate_segments")
+           "tq_decompress_aggregate_segments", "tq_mx_quantize", "tq_mx_quantize_both", "tq_mx_dequantize", "tq_mx_decompress_aggregate", "tq_mx_product",
+           "tq_mx_gated", "tq_mx_gated_backward")
 
 
 def _load_native(L: C.CDLL):
@@ -391,6 +416,108 @@ def tq_decompress_aggregate_apply(packed: torch.Tensor, d: int, params, theta: t
     """Aggregate the N packed rows and apply the SGD step in place on ``theta`` (and ``momentum_buf``)."""
     _check(_calls().decompress_aggregate_apply(packed, d, _params_array(params), weights, theta, momentum_buf, lr, momentum, weight_decay, stream), "tq_decompress_aggregate_apply")
     return theta
+
+
+# ---- microscaled 4-bit floating point ------------------------------------------------------------
+class MxMatrix:
+    """A [rows, cols] matrix of E2M1 codes with an E8M0 scale for every 32 elements of a row (tq_mx_t, include/tq.h).
+
+    ``codes`` is a uint8 tensor [rows, >= 16 * ceil(cols / 32)]; ``scales`` a uint8 tensor of ceil(rows / 128) rows (MX_TILES) or
+    ``rows`` rows (MX_ROWS).  Both may be views with any row stride that is a multiple of 16 bytes."""
+    __slots__ = ("codes", "scales", "rows", "cols", "layout")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, layout: int = MX_TILES):
+        self.codes, self.scales, self.rows, self.cols, self.layout = codes, scales, rows, cols, layout
+
+
+def tq_mx_code_stride(cols: int) -> int:
+    return int(lib().tq_mx_code_stride(cols))
+
+
+def tq_mx_scale_stride(cols: int, layout: int = MX_TILES) -> int:
+    return int(lib().tq_mx_scale_stride(cols, layout))
+
+
+def new_mx(rows: int, cols: int, layout: int = MX_TILES, device="cuda") -> MxMatrix:
+    """Memory for a matrix, uninitialised; the calls that write one write all of it, the filling of its last scale tiles included."""
+    blocks = (cols + 31) // 32
+    tiles = layout == MX_TILES
+    codes = torch.empty((rows, blocks * 16), dtype=torch.uint8, device=device)
+    scales = torch.empty(((rows + 127) // 128, (blocks + 3) // 4 * 512) if tiles else (rows, (blocks + 15) // 16 * 16), dtype=torch.uint8, device=device)
+    return MxMatrix(codes, scales, rows, cols, layout)
+
+
+def _seed(seed: int) -> int:
+    return seed & 0xFFFFFFFFFFFFFFFF
+
+
+def tq_mx_quantize(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int = 0, first_row: int = 0, cols: Optional[int] = None,
+                   layout: int = MX_TILES, out: Optional[MxMatrix] = None, stream=None) -> MxMatrix:
+    """Enqueue the quantisation of ``x`` ([rows, cols] or [cols], fp32 or bf16) along its rows; the first ``cols`` columns when given."""
+    if out is None:
+        out = new_mx(_rows(x), x.shape[-1] if cols is None else cols, layout, x.device)
+    _check(_calls().mx_quantize(x, rounding, _seed(seed), first_row, out, stream), "tq_mx_quantize")
+    return out
+
+
+def tq_mx_quantize_both(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int = 0, first_row: int = 0, out: Optional[MxMatrix] = None,
+                        out_t: Optional[MxMatrix] = None, stream=None) -> Tuple[MxMatrix, MxMatrix]:
+    """``x`` along its rows, and its transposed copy, whose blocks run along x's columns."""
+    if out is None:
+        out = new_mx(_rows(x), x.shape[-1], MX_TILES, x.device)
+    if out_t is None:
+        out_t = new_mx(out.cols, out.rows, MX_TILES, x.device)
+    _check(_calls().mx_quantize_both(x, rounding, _seed(seed), first_row, out, out_t, stream), "tq_mx_quantize_both")
+    return out, out_t
+
+
+def tq_mx_dequantize(m: MxMatrix, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values of ``m`` as a [rows, cols] tensor."""
+    if out is None:
+        out = torch.empty((m.rows, m.cols), dtype=dtype, device=m.codes.device)
+    _check(_calls().mx_dequantize(m, out, stream), "tq_mx_dequantize")
+    return out
+
+
+def tq_mx_decompress_aggregate(m: MxMatrix, weights: Optional[Sequence[float]] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue the mean (or weighted sum) of the rows of ``m`` (layout MX_ROWS); returns the [cols] fp32 update."""
+    if out is None:
+        out = torch.empty(m.cols, dtype=torch.float32, device=m.codes.device)
+    _check(_calls().mx_decompress_aggregate(m, weights, out, stream), "tq_mx_decompress_aggregate")
+    return out
+
+
+def tq_mx_product(a: MxMatrix, b: MxMatrix, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue a b^T; returns [a.rows, b.rows]."""
+    if out is None:
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.codes.device)
+    _check(_calls().mx_product(a, b, out, stream), "tq_mx_product")
+    return out
+
+
+def tq_mx_gated(x: MxMatrix, w_gate: MxMatrix, w_up: MxMatrix, activation: int = MX_SILU, projections: Optional[torch.Tensor] = None,
+                out: Optional[MxMatrix] = None, stream=None) -> MxMatrix:
+    """Enqueue act(x w_gate^T) * (x w_up^T), quantised along its rows.  ``projections``: a [tokens, 2 features] tensor that receives both
+    projections, for tq_mx_gated_backward."""
+    if out is None:
+        out = new_mx(x.rows, w_gate.rows, MX_TILES, x.codes.device)
+    _check(_calls().mx_gated(x, w_gate, w_up, activation, out, projections, stream), "tq_mx_gated")
+    return out
+
+
+def tq_mx_gated_backward(dh: torch.Tensor, projections: torch.Tensor, activation: int = MX_SILU, rounding: int = MX_STOCHASTIC, seed: int = 0,
+                         dgu: Optional[MxMatrix] = None, dgu_t: Optional[MxMatrix] = None, h_t: Optional[MxMatrix] = None,
+                         stream=None) -> Tuple[MxMatrix, MxMatrix, MxMatrix]:
+    """Enqueue the backward pass of tq_mx_gated up to the products; returns ([dg | du], its transposed copy, the transposed h)."""
+    tokens, features = _rows(dh), dh.shape[-1]
+    if dgu is None:
+        dgu = new_mx(tokens, 2 * features, MX_TILES, dh.device)
+    if dgu_t is None:
+        dgu_t = new_mx(2 * features, tokens, MX_TILES, dh.device)
+    if h_t is None:
+        h_t = new_mx(features, tokens, MX_TILES, dh.device)
+    _check(_calls().mx_gated_backward(dh, projections, activation, rounding, _seed(seed), dgu, dgu_t, h_t, stream), "tq_mx_gated_backward")
+    return dgu, dgu_t, h_t
 
 
 def tq_kernel_launches() -> int:

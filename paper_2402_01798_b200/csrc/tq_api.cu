@@ -355,6 +355,153 @@ tq_status tq_decompress_aggregate_segments(const uint32_t* packed_dev, size_t wo
     return TQ_OK;
 }
 
+// ---- microscaled 4-bit floating point -------------------------------------------------------------------
+
+size_t tq_mx_code_stride(uint64_t cols) { return static_cast<size_t>((cols + 31) / 32 * 16); }
+
+size_t tq_mx_scale_stride(uint64_t cols, tq_mx_layout layout) {
+    const uint64_t blocks = (cols + 31) / 32;
+    return static_cast<size_t>(layout == TQ_MX_TILES ? (blocks + 3) / 4 * 512 : (blocks + 15) / 16 * 16);
+}
+
+static tq_status check_mx(const tq_mx_t* m) {
+    if (!m || (m->layout != TQ_MX_TILES && m->layout != TQ_MX_ROWS)) return TQ_ERR_INVALID_ARG;
+    if (m->rows >= (1ull << 31) || m->cols > (1ull << 40)) return TQ_ERR_INVALID_ARG;
+    if (m->rows && m->cols && (!m->codes || !m->scales)) return TQ_ERR_INVALID_ARG;
+    if (!aligned(m->codes, 16) || !aligned(m->scales, 16) || m->code_stride % 16 != 0 || m->scale_stride % 16 != 0) return TQ_ERR_ALIGNMENT;
+    if (m->code_stride < tq_mx_code_stride(m->cols) || m->scale_stride < tq_mx_scale_stride(m->cols, static_cast<tq_mx_layout>(m->layout))) return TQ_ERR_BUFFER_TOO_SMALL;
+    if (m->code_stride >= (1ull << 40) || m->scale_stride >= (1ull << 40)) return TQ_ERR_INVALID_ARG;
+    return TQ_OK;
+}
+// launches count blocks in 31 bits: one for 128 x 128 elements, or for a row's 2048
+static bool mx_too_large(uint64_t rows, uint64_t cols) {
+    return (rows + 127) / 128 * ((cols + 127) / 128) >= (1ull << 31) || rows * ((cols + 2047) / 2048) >= (1ull << 31);
+}
+// a plain matrix of fp32 or bf16
+static tq_status check_plain(const void* x, tq_dtype dtype, uint64_t stride, uint64_t rows, uint64_t cols) {
+    if (dtype != TQ_F32 && dtype != TQ_BF16) return TQ_ERR_INVALID_ARG;
+    if (rows && cols && !x) return TQ_ERR_INVALID_ARG;
+    if (!aligned(x, elem_size(dtype))) return TQ_ERR_ALIGNMENT;
+    if (stride > (1ull << 40)) return TQ_ERR_INVALID_ARG;
+    return rows > 1 && stride < cols ? TQ_ERR_BUFFER_TOO_SMALL : TQ_OK;
+}
+// an operand of a product
+static tq_status check_operand(const tq_mx_t* m) {
+    if (tq_status s = check_mx(m)) return s;
+    return m->layout != TQ_MX_TILES || m->cols >= (1ull << 31) ? TQ_ERR_INVALID_ARG : TQ_OK;
+}
+
+static tq_status mx_quantize(const void* x_dev, tq_dtype dtype, uint64_t x_stride, tq_mx_rounding rounding, uint64_t seed, uint32_t first_row,
+                             const tq_mx_t* out, const tq_mx_t* out_t, void* stream) {
+    if (rounding != TQ_MX_NEAREST && rounding != TQ_MX_STOCHASTIC) return TQ_ERR_INVALID_ARG;
+    if (tq_status s = check_plain(x_dev, dtype, x_stride, out->rows, out->cols)) return s;
+    if (mx_too_large(out->rows, out->cols)) return TQ_ERR_INVALID_ARG;
+    if (out->rows == 0 || out->cols == 0) return TQ_OK;
+    const tq::MxQuantizeCall c{x_dev, dtype == TQ_BF16, x_stride, rounding == TQ_MX_STOCHASTIC, seed, first_row, out, out_t, static_cast<cudaStream_t>(stream)};
+    const cudaError_t e = tq::launch_mx_quantize(c);
+    if (e != cudaSuccess) return cuda_failed(e);
+    g_launches += 1;
+    return TQ_OK;
+}
+
+tq_status tq_mx_quantize(const void* x_dev, tq_dtype dtype, uint64_t x_stride, tq_mx_rounding rounding, uint64_t seed, uint32_t first_row,
+                         const tq_mx_t* out_host, void* stream) {
+    if (tq_status s = check_mx(out_host)) return s;
+    return mx_quantize(x_dev, dtype, x_stride, rounding, seed, first_row, out_host, nullptr, stream);
+}
+
+tq_status tq_mx_quantize_both(const void* x_dev, tq_dtype dtype, uint64_t x_stride, tq_mx_rounding rounding, uint64_t seed, uint32_t first_row,
+                              const tq_mx_t* out_host, const tq_mx_t* out_t_host, void* stream) {
+    if (tq_status s = check_mx(out_host)) return s;
+    if (tq_status s = check_mx(out_t_host)) return s;
+    if (out_t_host->rows != out_host->cols || out_t_host->cols != out_host->rows) return TQ_ERR_INVALID_ARG;
+    return mx_quantize(x_dev, dtype, x_stride, rounding, seed, first_row, out_host, out_t_host, stream);
+}
+
+tq_status tq_mx_dequantize(const tq_mx_t* m_host, void* out_dev, tq_dtype dtype, uint64_t out_stride, void* stream) {
+    if (tq_status s = check_mx(m_host)) return s;
+    if (tq_status s = check_plain(out_dev, dtype, out_stride, m_host->rows, m_host->cols)) return s;
+    if (mx_too_large(m_host->rows, m_host->cols)) return TQ_ERR_INVALID_ARG;
+    if (m_host->rows == 0 || m_host->cols == 0) return TQ_OK;
+    const cudaError_t e = tq::launch_mx_dequantize(*m_host, out_dev, dtype == TQ_BF16, out_stride, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_failed(e);
+    g_launches += 1;
+    return TQ_OK;
+}
+
+tq_status tq_mx_decompress_aggregate(const tq_mx_t* m_host, const float* weights_host, float* out_dev, void* stream) {
+    if (tq_status s = check_mx(m_host)) return s;
+    if (m_host->layout != TQ_MX_ROWS || m_host->rows == 0 || m_host->rows > TQ_MAX_WORKERS) return TQ_ERR_INVALID_ARG;
+    if (m_host->cols && !out_dev) return TQ_ERR_INVALID_ARG;
+    if (!aligned(out_dev, 32)) return TQ_ERR_ALIGNMENT;
+    if (m_host->cols == 0) return TQ_OK;
+    const cudaError_t e = tq::launch_mx_aggregate(*m_host, weights_host, out_dev, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_failed(e);
+    g_launches += 1;
+    return TQ_OK;
+}
+
+tq_status tq_mx_product(const tq_mx_t* a_host, const tq_mx_t* b_host, void* out_dev, tq_dtype dtype, uint64_t out_stride, void* stream) {
+    if (tq_status s = check_operand(a_host)) return s;
+    if (tq_status s = check_operand(b_host)) return s;
+    if (a_host->cols != b_host->cols) return TQ_ERR_INVALID_ARG;
+    const uint64_t m = a_host->rows, n = b_host->rows;
+    if (tq_status s = check_plain(out_dev, dtype, out_stride, m, n)) return s;
+    if (mx_too_large(m, n)) return TQ_ERR_INVALID_ARG;
+    if (m == 0 || n == 0) return TQ_OK;
+    if (a_host->cols == 0) {
+        const cudaError_t e = cudaMemset2DAsync(out_dev, (m > 1 ? out_stride : n) * elem_size(dtype), 0, n * elem_size(dtype), m, static_cast<cudaStream_t>(stream));
+        return e == cudaSuccess ? TQ_OK : cuda_failed(e);
+    }
+    const cudaError_t e = tq::launch_mx_product(*a_host, *b_host, out_dev, dtype == TQ_BF16, out_stride, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_failed(e);
+    g_launches += 1;
+    return TQ_OK;
+}
+
+tq_status tq_mx_gated(const tq_mx_t* x_host, const tq_mx_t* w_gate_host, const tq_mx_t* w_up_host, tq_mx_activation activation, const tq_mx_t* h_host,
+                      void* projections_dev, tq_dtype dtype, uint64_t proj_stride, void* stream) {
+    for (const tq_mx_t* m : {x_host, w_gate_host, w_up_host, h_host})
+        if (tq_status s = check_operand(m)) return s;
+    const uint64_t tokens = x_host->rows, features = w_gate_host->rows;
+    if (activation != TQ_MX_SILU && activation != TQ_MX_GELU) return TQ_ERR_INVALID_ARG;
+    if (w_up_host->rows != features || w_gate_host->cols != x_host->cols || w_up_host->cols != x_host->cols) return TQ_ERR_INVALID_ARG;
+    if (h_host->rows != tokens || h_host->cols != features || features % 32 != 0 || x_host->cols == 0) return TQ_ERR_INVALID_ARG;
+    if (projections_dev) {
+        if (tq_status s = check_plain(projections_dev, dtype, proj_stride, tokens, 2 * features)) return s;
+    }
+    if (mx_too_large(tokens, features)) return TQ_ERR_INVALID_ARG;
+    if (tokens == 0 || features == 0) return TQ_OK;
+    const tq::MxGatedCall c{x_host, w_gate_host, w_up_host, h_host, activation == TQ_MX_GELU, projections_dev, dtype == TQ_BF16, proj_stride,
+                            static_cast<cudaStream_t>(stream)};
+    const cudaError_t e = tq::launch_mx_gated(c);
+    if (e != cudaSuccess) return cuda_failed(e);
+    g_launches += 1;
+    return TQ_OK;
+}
+
+tq_status tq_mx_gated_backward(const void* dh_dev, uint64_t dh_stride, const void* projections_dev, uint64_t proj_stride, tq_dtype dtype,
+                               tq_mx_activation activation, tq_mx_rounding rounding, uint64_t seed, const tq_mx_t* dgu_host, const tq_mx_t* dgu_t_host,
+                               const tq_mx_t* h_t_host, void* stream) {
+    for (const tq_mx_t* m : {dgu_host, dgu_t_host, h_t_host})
+        if (tq_status s = check_mx(m)) return s;
+    if (activation != TQ_MX_SILU && activation != TQ_MX_GELU) return TQ_ERR_INVALID_ARG;
+    if (rounding != TQ_MX_NEAREST && rounding != TQ_MX_STOCHASTIC) return TQ_ERR_INVALID_ARG;
+    const uint64_t tokens = dgu_host->rows, features = h_t_host->rows;
+    if (features % 32 != 0 || dgu_host->cols != 2 * features || dgu_t_host->rows != 2 * features || dgu_t_host->cols != tokens || h_t_host->cols != tokens)
+        return TQ_ERR_INVALID_ARG;
+    if (tq_status s = check_plain(dh_dev, dtype, dh_stride, tokens, features)) return s;
+    if (tq_status s = check_plain(projections_dev, dtype, proj_stride, tokens, 2 * features)) return s;
+    if (mx_too_large(tokens, features)) return TQ_ERR_INVALID_ARG;
+    if (tokens == 0 || features == 0) return TQ_OK;
+    const tq::MxGatedBackwardCall c{dh_dev, projections_dev, dtype == TQ_BF16, dh_stride, proj_stride, activation == TQ_MX_GELU, rounding == TQ_MX_STOCHASTIC, seed,
+                                    dgu_host, dgu_t_host, h_t_host, static_cast<cudaStream_t>(stream)};
+    const cudaError_t e = tq::launch_mx_gated_backward(c);
+    if (e != cudaSuccess) return cuda_failed(e);
+    g_launches += 1;
+    return TQ_OK;
+}
+
 const char* tq_strerror(tq_status s) {
     switch (s) {
         case TQ_OK: return "ok";
@@ -374,10 +521,11 @@ uint64_t tq_kernel_launches(void) { return g_launches.load(); }
 
 tq_status tq_wait_expired_count(uint32_t* count_host) {
     if (!count_host) return TQ_ERR_INVALID_ARG;
-    unsigned int n = 0;
-    const cudaError_t e = tq::read_wait_expired(&n);
+    unsigned int n = 0, of_products = 0;
+    cudaError_t e = tq::read_wait_expired(&n);
+    if (e == cudaSuccess) e = tq::read_product_wait_expired(&of_products);
     if (e != cudaSuccess) return cuda_failed(e);
-    *count_host = n;
+    *count_host = n + of_products;
     return TQ_OK;
 }
 

@@ -148,4 +148,31 @@ bool params_request_ok(uint32_t num_levels, int mode, int rule, uint32_t* bits);
 cudaError_t launch_params_device(const tq_stats_t* stats_dev, uint32_t n, uint32_t num_levels, uint32_t bits, uint32_t mode,
                                  double gamma, int rule, double alpha_user, tq_params_t* params_dev, cudaStream_t stream);
 
+// ---- microscaled 4-bit floating point ----------------------------------------------------------------------
+struct MxQuantizeCall {
+    const void* x; bool bf16; uint64_t x_stride;
+    bool stochastic; uint64_t seed; uint32_t first_row;
+    const tq_mx_t* out; const tq_mx_t* out_t;        // out_t may be null
+    cudaStream_t stream;
+};
+cudaError_t launch_mx_quantize(const MxQuantizeCall& c);
+cudaError_t launch_mx_dequantize(const tq_mx_t& m, void* out, bool bf16, uint64_t stride, cudaStream_t stream);
+cudaError_t launch_mx_aggregate(const tq_mx_t& m, const float* weights, float* out, cudaStream_t stream);
+cudaError_t launch_mx_product(const tq_mx_t& a, const tq_mx_t& b, void* out, bool bf16, uint64_t out_stride, cudaStream_t stream);
+struct MxGatedCall {
+    const tq_mx_t *x, *w_gate, *w_up, *h;
+    bool gelu;
+    void* projections; bool proj_bf16; uint64_t proj_stride;      // projections may be null
+    cudaStream_t stream;
+};
+cudaError_t launch_mx_gated(const MxGatedCall& c);
+struct MxGatedBackwardCall {
+    const void *dh, *gu; bool bf16; uint64_t dh_stride, gu_stride;
+    bool gelu, stochastic; uint64_t seed;
+    const tq_mx_t *dgu, *dgu_t, *h_t;
+    cudaStream_t stream;
+};
+cudaError_t launch_mx_gated_backward(const MxGatedBackwardCall& c);
+cudaError_t read_product_wait_expired(unsigned int* count);       // as read_wait_expired, of the products
+
 }  // namespace tq

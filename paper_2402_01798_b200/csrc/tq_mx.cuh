@@ -1,0 +1,166 @@
+// Microscaled 4-bit floating point on the device: scales, codes and where they lie (format: include/tq.h).
+#pragma once
+#include "tq_device.cuh"
+
+namespace tq {
+
+// One MX matrix as a kernel sees it.
+struct MxView {
+    uint8_t* codes;
+    uint8_t* scales;
+    uint64_t rows, cols, code_stride, scale_stride;
+    uint32_t tiles;                // layout of the scales: 1 tiles, 0 row after row
+};
+inline MxView mx_view(const tq_mx_t& m) {
+    return MxView{m.codes, m.scales, m.rows, m.cols, m.code_stride, m.scale_stride, m.layout == TQ_MX_TILES};
+}
+__host__ __device__ __forceinline__ uint64_t mx_blocks(uint64_t cols) { return (cols + 31) / 32; }
+__device__ __forceinline__ uint64_t mx_scale_at(const MxView& m, uint64_t row, uint64_t block) {
+    if (!m.tiles) return row * m.scale_stride + block;
+    return (row >> 7) * m.scale_stride + (block >> 2) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
+}
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// max(|a|, |b|, |c|), NaN if one is
+__device__ __forceinline__ float max_abs3(float a, float b, float c) {
+    float r; asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r;
+}
+__device__ __forceinline__ float max_abs_32(const float (&v)[32]) {
+    float m[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = max_abs3(v[4 * i], v[4 * i + 1], v[4 * i + 2]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = max_abs3(m[i], m[i + 4], v[4 * i + 3]);
+    m[0] = max_abs3(m[0], v[19], v[23]);
+    m[1] = max_abs3(m[1], v[27], v[31]);
+    m[2] = max_abs3(m[2], m[3], m[0]);
+    return max_abs3(m[1], m[2], 0.0f);
+}
+
+// The scale byte of a block whose largest magnitude is `top`; 255 where the block holds a NaN or an infinity.
+//   nearest:    2^(floor(log2 top) - 2): top / scale lies in [4, 8), what exceeds 6 is rounded to 6;
+//   stochastic: the smallest power of two with top <= 6 scale, so that nothing is cut off and the expectation is the element.
+//               With top = m 2^e that is e - 2 for m <= 3/2 and e - 1 above: the carry of 0x3FFFFF into the exponent.
+template <bool STOCHASTIC>
+__device__ __forceinline__ uint32_t mx_scale_byte(float top) {
+    const uint32_t p = __float_as_uint(top);
+    const int e = static_cast<int>((STOCHASTIC ? p + 0x3FFFFFu : p) >> 23) - 2;
+    return p >= kInfBits ? 255u : static_cast<uint32_t>(e > 0 ? e : 0);
+}
+// 1 / scale, exact: 2^(127 - byte), a normal number for every byte that mx_scale_byte gives a finite block (0 .. 253)
+__device__ __forceinline__ float mx_inv_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ float mx_scale_value(uint32_t byte) {
+    return __uint_as_float(byte == 255u ? 0x7FC00000u : byte == 0u ? 0x00400000u : byte << 23);
+}
+
+// Two scaled elements -> two codes in the low byte, to nearest, ties to even, 6 at most.
+__device__ __forceinline__ uint32_t e2m1_nearest8(const float (&v)[8]) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+
+// One scaled element y (|y| <= 6), rounded up when its 16 random bits r are below rint(p 2^16): with the grid's step h (1/2 below 2, 1
+// below 4, 2 above) and u = |y| / h = k + p, the integer rint(u 2^16) + 65535 - r carries into bit 16 exactly then.  The code of
+// k is k + 2 log2(2h): that is added in the same place.  `not_r` holds 65535 - r in its low 16 bits, zeros above.
+__device__ __forceinline__ uint32_t e2m1_stochastic(float y, uint32_t not_r) {
+    const uint32_t bits = __float_as_uint(y);
+    const int exponent = static_cast<int>(bits & kInfBits);
+    const int eb = exponent > 0x3F800000 ? exponent : 0x3F800000;          // of max(|y|, 1): 127, 128, 129 for h = 1/2, 1, 2
+    const float up = __uint_as_float(0x87800000u - static_cast<uint32_t>(eb));   // 2^16 / h = 2^(17 - log2(2h)); 0x87800000 = 271 << 23
+    const uint32_t v = __float_as_uint(fmaf(fabsf(y), up, kMagic));        // the product is exact; one rounding, to an integer
+    const uint32_t s = v + ((static_cast<uint32_t>(eb) - 0x3F800000u) >> 6) + not_r;
+    return ((s >> 16) & 7u) | ((bits >> 28) & 8u);
+}
+__device__ __forceinline__ uint32_t e2m1_stochastic8(const float (&y)[8], const uint32_t (&random)[4]) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t n = ~random[i];
+        r |= e2m1_stochastic(y[2 * i], n & 0xFFFFu) << (8 * i);
+        r |= e2m1_stochastic(y[2 * i + 1], n >> 16) << (8 * i + 4);
+    }
+    return r;
+}
+
+// Eight codes -> fp32, before the scale.
+__device__ __forceinline__ void e2m1_values8(uint32_t codes, float (&v)[8]) {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(v[2 * i]), "=f"(v[2 * i + 1]) : "r"(h[i]));
+}
+
+// Random bits of the elements (row, 8 * group .. 8 * group + 7): word i holds those of elements 2i (low half) and 2i + 1.
+__device__ __forceinline__ void mx_random8(uint32_t row, uint64_t group, const RoundKeys& keys, uint32_t (&out)[4]) {
+    const PhiloxRun run = philox_run(static_cast<uint32_t>(group >> 32), row, keys);
+    philox_block(static_cast<uint32_t>(group), run, keys, out);
+}
+
+// 32 elements -> their 32 codes, element 0 in the lowest nibble.  `random(q, out)` gives the bits of elements 8q .. 8q + 7.
+template <bool STOCHASTIC, class Random>
+__device__ __forceinline__ uint4 mx_encode32(const float (&v)[32], uint32_t byte, Random random) {
+    uint32_t w[4];
+    const float inv = mx_inv_scale(byte);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = v[8 * q + e] * inv;
+        if constexpr (STOCHASTIC) {
+            uint32_t r[4];
+            random(q, r);
+            w[q] = e2m1_stochastic8(y, r);
+        } else {
+            w[q] = e2m1_nearest8(y);
+        }
+        w[q] = byte == 255u ? 0u : w[q];
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r;
+}
+__device__ __forceinline__ void stg128(void* p, uint4 v) {
+    asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 ldg128(const void* p) {
+    uint4 v; asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory"); return v;
+}
+__device__ __forceinline__ uint32_t ldg8(const void* p) {
+    uint32_t v; asm volatile("ld.global.b8 %0, [%1];" : "=r"(v) : "l"(p) : "memory"); return v;
+}
+
+// ---- activations of the gated block ------------------------------------------------------------------------
+// x * s with s = sigmoid(z): SiLU has z = x, the tanh form of GELU z = 2 sqrt(2/pi) (x + 0.044715 x^3), since
+// (1 + tanh t) / 2 = sigmoid(2 t).
+constexpr float kGeluC = 1.5957691216057308f;      // 2 sqrt(2/pi)
+constexpr float kGeluB = 0.044715f;
+template <bool GELU>
+__device__ __forceinline__ float gate_sigmoid(float x) {
+    float z = x;
+    if constexpr (GELU) z = kGeluC * x * fmaf(kGeluB * x, x, 1.0f);
+    return __fdividef(1.0f, 1.0f + __expf(-z));
+}
+template <bool GELU>
+__device__ __forceinline__ float gate_value(float x) { return x * gate_sigmoid<GELU>(x); }
+// value and derivative: s + x z' s (1 - s)
+template <bool GELU>
+__device__ __forceinline__ void gate_value_slope(float x, float& value, float& slope) {
+    const float s = gate_sigmoid<GELU>(x);
+    float dz = 1.0f;
+    if constexpr (GELU) dz = fminf(kGeluC * fmaf(3.0f * kGeluB * x, x, 1.0f), 1e30f);    // where it would overflow, s is 0 or 1
+    value = x * s;
+    slope = fmaf(value * (1.0f - s), dz, s);
+}
+
+}  // namespace tq

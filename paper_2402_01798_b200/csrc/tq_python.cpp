@@ -9,6 +9,7 @@
 
 #include <cstring>
 #include <exception>
+#include <string>
 #include <vector>
 
 #include "tq.h"
@@ -31,6 +32,13 @@ struct Functions {
     decltype(&tq_stats_hinted_segments) stats_hinted_segments;
     decltype(&tq_compress_segments) compress_segments;
     decltype(&tq_decompress_aggregate_segments) decompress_aggregate_segments;
+    decltype(&tq_mx_quantize) mx_quantize;
+    decltype(&tq_mx_quantize_both) mx_quantize_both;
+    decltype(&tq_mx_dequantize) mx_dequantize;
+    decltype(&tq_mx_decompress_aggregate) mx_decompress_aggregate;
+    decltype(&tq_mx_product) mx_product;
+    decltype(&tq_mx_gated) mx_gated;
+    decltype(&tq_mx_gated_backward) mx_gated_backward;
 } F;
 
 struct Failed {};                              // a Python exception is set
@@ -371,6 +379,128 @@ tq_status decompress_aggregate_segments(Args& a) {           // packed, segments
                                            a.stream());
 }
 
+// ---- microscaled 4-bit floating point: an MxMatrix (binding.py) is five attributes --------------------------------
+struct MxNames {
+    PyObject *codes, *scales, *rows, *cols, *layout;
+} N;
+
+// Kernels run on the current device and take addresses of no other.
+void on_current_device(const at::Tensor& t, const char* what) {
+    if (!t.is_cuda()) fail(PyExc_ValueError, (std::string(what) + " must be a CUDA tensor").c_str());
+    if (t.device().index() != c10::cuda::current_device()) fail(PyExc_ValueError, (std::string(what) + " is not on the current device").c_str());
+}
+uint64_t attribute(PyObject* o, PyObject* name) {
+    PyObject* v = PyObject_GetAttr(o, name);
+    if (!v) throw Failed();
+    const uint64_t x = PyLong_AsUnsignedLongLong(v);               // refuses what is negative or no whole number
+    Py_DECREF(v);
+    if (x == ~0ull && PyErr_Occurred()) throw Failed();
+    return x;
+}
+// The bytes of one attribute: `rows` rows of at least `width` bytes, wherever they start.
+uint8_t* bytes_of(PyObject* o, PyObject* name, const char* what, uint64_t rows, uint64_t width, uint64_t* stride) {
+    PyObject* v = PyObject_GetAttr(o, name);
+    if (!v) throw Failed();
+    Py_DECREF(v);                                                  // held by the matrix, which the caller's arguments hold
+    if (!THPVariable_Check(v)) fail(PyExc_TypeError, "codes and scales must be tensors");
+    const at::Tensor& t = THPVariable_Unpack(v);
+    on_current_device(t, what);
+    if (t.scalar_type() != at::kByte || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) fail(PyExc_TypeError, "codes and scales must be [rows, bytes] uint8 with unit inner stride");
+    if (static_cast<uint64_t>(t.size(0)) < rows || (rows && static_cast<uint64_t>(t.size(1)) < width)) fail(PyExc_ValueError, "codes or scales are smaller than the matrix");
+    *stride = t.size(0) > 1 ? static_cast<uint64_t>(t.stride(0)) : static_cast<uint64_t>(t.size(1)) / 16 * 16;
+    return static_cast<uint8_t*>(t.data_ptr());
+}
+tq_mx_t mx(Args& a) {
+    PyObject* o = a.next();
+    tq_mx_t m{};
+    m.rows = attribute(o, N.rows); m.cols = attribute(o, N.cols);
+    m.layout = static_cast<uint32_t>(attribute(o, N.layout));
+    const uint64_t blocks = m.cols / 32 + (m.cols % 32 != 0);
+    const bool tiles = m.layout == TQ_MX_TILES;
+    m.codes = bytes_of(o, N.codes, "codes", m.rows, blocks * 16, &m.code_stride);
+    m.scales = bytes_of(o, N.scales, "scales", tiles ? m.rows / 128 + (m.rows % 128 != 0) : m.rows, tiles ? (blocks + 3) / 4 * 512 : (blocks + 15) / 16 * 16, &m.scale_stride);
+    return m;
+}
+// A plain [rows, cols] tensor, fp32 or bf16; a vector is one row.  At least `rows` x `cols` where those are given.
+struct Plain {
+    void* data;
+    tq_dtype dtype;
+    uint64_t stride;
+};
+Plain plain(const at::Tensor& t, const char* what, uint64_t rows, uint64_t cols) {
+    on_current_device(t, what);
+    const int64_t dims = t.dim();
+    if ((dims != 1 && dims != 2) || (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1)) fail(PyExc_ValueError, (std::string(what) + " must be [rows, cols] with unit inner stride").c_str());
+    Plain p;
+    if (t.scalar_type() == at::kFloat) p.dtype = TQ_F32;
+    else if (t.scalar_type() == at::kBFloat16) p.dtype = TQ_BF16;
+    else fail(PyExc_TypeError, (std::string(what) + " must be float32 or bfloat16").c_str());
+    const uint64_t have = dims == 2 ? static_cast<uint64_t>(t.size(0)) : 1u, wide = static_cast<uint64_t>(t.size(dims - 1));
+    if (have < rows || wide < cols) fail(PyExc_ValueError, (std::string(what) + " is smaller than the call needs").c_str());
+    if (have > 1 && rows > 1 && t.stride(0) < static_cast<int64_t>(cols)) fail(PyExc_ValueError, (std::string(what) + " has rows that overlap").c_str());
+    p.data = t.data_ptr();
+    p.stride = have > 1 ? static_cast<uint64_t>(t.stride(0)) : wide;
+    return p;
+}
+tq_status mx_quantize(Args& a) {                // x, rounding, seed, first_row, out, stream
+    const at::Tensor& x = a.tensor();
+    const uint32_t rounding = a.u32();
+    const uint64_t seed = a.u64();
+    const uint32_t first = a.u32();
+    const tq_mx_t out = mx(a);
+    const Plain p = plain(x, "x", out.rows, out.cols);
+    return call(F.mx_quantize, p.data, p.dtype, p.stride, static_cast<tq_mx_rounding>(rounding), seed, first, &out, a.stream());
+}
+tq_status mx_quantize_both(Args& a) {           // x, rounding, seed, first_row, out, out_t, stream
+    const at::Tensor& x = a.tensor();
+    const uint32_t rounding = a.u32();
+    const uint64_t seed = a.u64();
+    const uint32_t first = a.u32();
+    const tq_mx_t out = mx(a), out_t = mx(a);
+    const Plain p = plain(x, "x", out.rows, out.cols);
+    return call(F.mx_quantize_both, p.data, p.dtype, p.stride, static_cast<tq_mx_rounding>(rounding), seed, first, &out, &out_t, a.stream());
+}
+tq_status mx_dequantize(Args& a) {              // matrix, out, stream
+    const tq_mx_t m = mx(a);
+    const Plain p = plain(a.tensor(), "out", m.rows, m.cols);
+    return call(F.mx_dequantize, &m, p.data, p.dtype, p.stride, a.stream());
+}
+tq_status mx_decompress_aggregate(Args& a) {    // matrix, weights, out, stream
+    const tq_mx_t m = mx(a);
+    const float* w = a.weights(static_cast<uint32_t>(m.rows < TQ_MAX_WORKERS ? m.rows : TQ_MAX_WORKERS));
+    const Plain p = plain(a.tensor(), "out", 1, m.cols);
+    if (p.dtype != TQ_F32) fail(PyExc_TypeError, "out must be float32");
+    return call(F.mx_decompress_aggregate, &m, w, static_cast<float*>(p.data), a.stream());
+}
+tq_status mx_product(Args& a) {                 // a, b, out, stream
+    const tq_mx_t x = mx(a), y = mx(a);
+    const Plain p = plain(a.tensor(), "out", x.rows, y.rows);
+    return call(F.mx_product, &x, &y, p.data, p.dtype, p.stride, a.stream());
+}
+tq_status mx_gated(Args& a) {                   // x, w_gate, w_up, activation, h, projections, stream
+    const tq_mx_t x = mx(a), wg = mx(a), wu = mx(a);
+    const uint32_t act = a.u32();
+    const tq_mx_t h = mx(a);
+    PyObject* o = a.next();
+    Plain p{nullptr, TQ_F32, 0};
+    if (o != Py_None) {
+        if (!THPVariable_Check(o)) fail(PyExc_TypeError, "a tensor is needed");
+        p = plain(THPVariable_Unpack(o), "projections", x.rows, 2 * wg.rows);
+    }
+    return call(F.mx_gated, &x, &wg, &wu, static_cast<tq_mx_activation>(act), &h, p.data, p.dtype, p.stride, a.stream());
+}
+tq_status mx_gated_backward(Args& a) {          // dh, projections, activation, rounding, seed, dgu, dgu_t, h_t, stream
+    const at::Tensor& dh = a.tensor();
+    const at::Tensor& gu = a.tensor();
+    const uint32_t act = a.u32(), rounding = a.u32();
+    const uint64_t seed = a.u64();
+    const tq_mx_t dgu = mx(a), dgu_t = mx(a), h_t = mx(a);
+    const Plain p = plain(dh, "dh", dgu.rows, h_t.rows), q = plain(gu, "projections", dgu.rows, dgu.cols);
+    if (p.dtype != q.dtype) fail(PyExc_TypeError, "dh and projections must be of one type");
+    return call(F.mx_gated_backward, p.data, p.stride, q.data, q.stride, p.dtype, static_cast<tq_mx_activation>(act), static_cast<tq_mx_rounding>(rounding), seed, &dgu, &dgu_t,
+                &h_t, a.stream());
+}
+
 template <tq_status (*CALL)(Args&)>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     try {
@@ -404,9 +534,15 @@ PyMethodDef methods[] = {
     TQ_ENTRY(stats), TQ_ENTRY(stats_hinted), TQ_ENTRY(stats_static), TQ_ENTRY(params_batch), TQ_ENTRY(params_device), TQ_ENTRY(compress),
     TQ_ENTRY(compress_device_params), TQ_ENTRY(decompress_aggregate), TQ_ENTRY(decompress_aggregate_rows), TQ_ENTRY(decompress_aggregate_apply),
     TQ_ENTRY(decompress_aggregate_device_params), TQ_ENTRY(stats_segments), TQ_ENTRY(stats_hinted_segments), TQ_ENTRY(compress_segments),
-    TQ_ENTRY(decompress_aggregate_segments), {nullptr, nullptr, 0, nullptr}};
+    TQ_ENTRY(decompress_aggregate_segments), TQ_ENTRY(mx_quantize), TQ_ENTRY(mx_quantize_both), TQ_ENTRY(mx_dequantize), TQ_ENTRY(mx_decompress_aggregate),
+    TQ_ENTRY(mx_product), TQ_ENTRY(mx_gated), TQ_ENTRY(mx_gated_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module{PyModuleDef_HEAD_INIT, "_tq_python", "Argument marshalling for libtq.so.", -1, methods};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tq_python() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__tq_python() {
+    N = MxNames{PyUnicode_InternFromString("codes"), PyUnicode_InternFromString("scales"), PyUnicode_InternFromString("rows"), PyUnicode_InternFromString("cols"),
+                PyUnicode_InternFromString("layout")};
+    if (!N.codes || !N.scales || !N.rows || !N.cols || !N.layout) return nullptr;
+    return PyModule_Create(&module);
+}
