@@ -66,26 +66,34 @@ __device__ __forceinline__ uint32_t e2m1_nearest8(const float (&v)[8]) {
 }
 
 // One scaled element y (|y| <= 6), rounded up when its 16 random bits r are below rint(p 2^16): with the grid's step h (1/2 below 2, 1
-// below 4, 2 above) and u = |y| / h = k + p, the integer rint(u 2^16) + 65535 - r carries into bit 16 exactly then.  The code of
-// k is k + 2 log2(2h): that is added in the same place.  `not_r` holds 65535 - r in its low 16 bits, zeros above.
-__device__ __forceinline__ uint32_t e2m1_stochastic(float y, uint32_t not_r) {
-    const uint32_t bits = __float_as_uint(y);
-    const int exponent = static_cast<int>(bits & kInfBits);
-    const int eb = exponent > 0x3F800000 ? exponent : 0x3F800000;          // of max(|y|, 1): 127, 128, 129 for h = 1/2, 1, 2
-    const float up = __uint_as_float(0x87800000u - static_cast<uint32_t>(eb));   // 2^16 / h = 2^(17 - log2(2h)); 0x87800000 = 271 << 23
-    const uint32_t v = __float_as_uint(fmaf(fabsf(y), up, kMagic));        // the product is exact; one rounding, to an integer
-    const uint32_t s = v + ((static_cast<uint32_t>(eb) - 0x3F800000u) >> 6) + not_r;
-    return ((s >> 16) & 7u) | ((bits >> 28) & 8u);
+// below 4, 2 above) and u = |y| / h = k + p, the integer rint(u 2^16) + 65535 - r carries into bit 16 exactly then.  The code of k is
+// k + 2 log2(2h), which is added in the same place; byte 2 of the result is the code without its sign (above it nothing is cleared).
+// Seven operations: `eb` is the exponent of max(|y|, 1) with 65535 << 6 in the mantissa, so that one shift brings the code of the step to
+// bit 17 and 65535 to bit 0; and the 254 << 16 that the exponent's bias adds there is made up to 2^24 by 2 << 16 in the magic number.
+constexpr int kOnes = 65535 << 6;
+template <bool ODD>
+__device__ __forceinline__ uint32_t e2m1_stochastic(float y, uint32_t random) {
+    const int exponent = static_cast<int>((__float_as_uint(y) & kInfBits) | kOnes);
+    const int eb = max(exponent, 0x3F800000 | kOnes);
+    const float up = __uint_as_float(0x87800000u + kOnes - static_cast<uint32_t>(eb));     // 2^16 / h = 2^(17 - log2(2h)); 0x87800000 = 271 << 23
+    const uint32_t v = __float_as_uint(fmaf(fabsf(y), up, kMagic + 131072.0f));            // the product is exact; one rounding, to an integer
+    return dot_halves_signed(random, ODD ? 0xFF00u : 0x00FFu, v + (static_cast<uint32_t>(eb) >> 6));
+}
+// Byte 3 of four words.
+__device__ __forceinline__ uint32_t byte3_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073u), __byte_perm(c, d, 0x0073u), 0x5410u);
 }
 __device__ __forceinline__ uint32_t e2m1_stochastic8(const float (&y)[8], const uint32_t (&random)[4]) {
-    uint32_t r = 0;
+    uint32_t s[8], x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __float_as_uint(y[i]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t n = ~random[i];
-        r |= e2m1_stochastic(y[2 * i], n & 0xFFFFu) << (8 * i);
-        r |= e2m1_stochastic(y[2 * i + 1], n >> 16) << (8 * i + 4);
+        s[2 * i] = e2m1_stochastic<false>(y[2 * i], random[i]);
+        s[2 * i + 1] = e2m1_stochastic<true>(y[2 * i + 1], random[i]);
     }
-    return r;
+    const uint32_t even = byte3_of(x[0], x[2], x[4], x[6]), odd = byte3_of(x[1], x[3], x[5], x[7]);
+    return pack_byte2<4>(s) | ((even >> 4) & 0x08080808u) | (odd & 0x80808080u);
 }
 
 // Eight codes -> fp32, before the scale.
@@ -114,7 +122,7 @@ __device__ __forceinline__ uint4 mx_encode32(const float (&v)[32], uint32_t byte
     for (int q = 0; q < 4; ++q) {
         float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = v[8 * q + e] * inv;
+        for (int e = 0; e < 8; e += 2) unpair(mul2(pair(v[8 * q + e], v[8 * q + e + 1]), both(inv)), y[e], y[e + 1]);
         if constexpr (STOCHASTIC) {
             uint32_t r[4];
             random(q, r);

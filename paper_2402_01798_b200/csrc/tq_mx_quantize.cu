@@ -12,6 +12,28 @@ struct MxInput {
     uint32_t wide;                 // 1: every row starts on a 16-byte boundary
 };
 
+// A row block of 32 elements of the matrix from memory, zeros outside.  `wide`: the row starts on a 16-byte boundary.
+template <bool BF16>
+__device__ __forceinline__ void load_row_block(const void* data, uint64_t at, bool wide, int count, float (&v)[32]) {
+    const char* src = static_cast<const char*>(data) + at * (BF16 ? 2 : 4);
+    if (wide && count >= 32) {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 4 : 8); ++i) {
+            const uint4 w = ldg128(src + 16 * i);
+            if constexpr (BF16) {
+                const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { v[8 * i + 2 * k] = __uint_as_float(x[k] << 16); v[8 * i + 2 * k + 1] = __uint_as_float(x[k] & 0xFFFF0000u); }
+            } else {
+                v[4 * i] = __uint_as_float(w.x); v[4 * i + 1] = __uint_as_float(w.y); v[4 * i + 2] = __uint_as_float(w.z); v[4 * i + 3] = __uint_as_float(w.w);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = i < count ? load1<BF16>(src, i) : 0.0f;
+    }
+}
+
 // ---- along the rows ----------------------------------------------------------------------------------------
 // One thread makes one block: 64 or 128 bytes in, 16 bytes of codes and a byte of scale out, no exchange between threads.
 // A block of 256 threads covers 2^shift MX blocks of 256 >> shift rows.  Bound by memory where rounding is to nearest.
@@ -26,24 +48,8 @@ __global__ void __launch_bounds__(kThreads) mx_rows_kernel(MxInput in, MxView ou
         if (out.tiles && row < (out.rows + 127) / 128 * 128 && block < (blocks + 3) / 4 * 4) out.scales[mx_scale_at(out, row, block)] = 0;
         return;
     }
-    const char* src = static_cast<const char*>(in.data) + (row * in.stride + block * 32) * (BF16 ? 2 : 4);
     float v[32];
-    if (block * 32 + 32 <= out.cols) {
-#pragma unroll
-        for (int i = 0; i < (BF16 ? 4 : 8); ++i) {
-            const uint4 w = ldg128(src + 16 * i);
-            if constexpr (BF16) {
-                const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) { v[8 * i + 2 * k] = __uint_as_float(x[k] << 16); v[8 * i + 2 * k + 1] = __uint_as_float(x[k] & 0xFFFF0000u); }
-            } else {
-                v[4 * i] = __uint_as_float(w.x); v[4 * i + 1] = __uint_as_float(w.y); v[4 * i + 2] = __uint_as_float(w.z); v[4 * i + 3] = __uint_as_float(w.w);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = block * 32 + i < out.cols ? load1<BF16>(src, i) : 0.0f;
-    }
+    load_row_block<BF16>(in.data, row * in.stride + block * 32, true, out.cols - block * 32 < 32 ? static_cast<int>(out.cols - block * 32) : 32, v);
     const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
     const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&r)[4]) { mx_random8(first_row + static_cast<uint32_t>(row), block * 4 + q, keys, r); });
     stg128(out.codes + row * out.code_stride + block * 16, codes);
@@ -51,127 +57,113 @@ __global__ void __launch_bounds__(kThreads) mx_rows_kernel(MxInput in, MxView ou
 }
 
 // ---- tiles in shared memory ------------------------------------------------------------------------------------
-// 128 x 128 elements in fp32.  32 elements are followed by 4 words of padding: a thread that reads 32 elements of a row in
-// 16-byte steps then meets no other thread of its quarter warp in a bank, and neither do 32 threads that read down 32 columns.
-constexpr int kTile = 128;
+// 64 x 128 elements, one block of 32 along a row and one along a column for each of 256 threads.  The thread makes its row block from
+// registers and leaves the elements in shared memory in fp32 for the thread that makes the column block.  32 elements are followed by
+// 4 words of padding: the 16-byte accesses of eight threads (two rows, four blocks) then touch different banks, as do those of 32
+// threads down 32 columns.  53 KB with the random bits: four blocks an SM, so that loads of one run beside the arithmetic of others.
+constexpr int kTileRows = 64, kTileCols = 128;
 constexpr int kTilePitch = 4 * 36;
 struct MxTile {
-    float v[kTile * kTilePitch];
-    uint32_t random[kTile * 64];           // 16 bits an element, in 16-byte chunks of 8; see random_chunk
+    float v[kTileRows * kTilePitch];
+    uint32_t random[kTileRows * 64];       // 16 bits an element, in 16-byte chunks of 8; see random_chunk
 };
 __device__ __forceinline__ int tile_at(int r, int c) { return r * kTilePitch + (c >> 5) * 36 + (c & 31); }
 // Word of the 16-byte chunk with the bits of row r, columns 8g .. 8g + 7.  The exchange of chunks keeps eight threads that write (two rows,
 // four blocks) in different banks.
 __device__ __forceinline__ int random_chunk(int r, int g) { return r * 64 + ((g ^ ((g >> 3) | ((r & 1) << 1))) << 2); }
 
-// Codes and scales of the tile's rows: rows r0 .., columns c0 .. of the matrix `out`, both multiples of 32; `width` columns of the tile count
-// and `height` rows.  `fill`: the tile ends the matrix on the right, and its row of scales is filled up with zeros.
-template <bool STOCHASTIC, bool KEEP>
-__device__ __forceinline__ void tile_rows(MxTile& t, const MxView& out, uint64_t r0, uint64_t c0, int height, int width, bool fill, const RoundKeys& keys,
-                                          uint32_t first_row, uint64_t random_c0) {
-    const uint64_t blocks = mx_blocks(out.cols);
-    for (int item = threadIdx.x; item < kTile * 4; item += blockDim.x) {
-        const int r = item >> 2, b = item & 3;
-        const uint64_t block = c0 / 32 + b;
-        const bool inside = r < height && b * 32 < width;
-        float v[32];
+// This thread's row block: row r, block b of the tile.
+struct MxItem {
+    int r, b;
+};
+__device__ __forceinline__ MxItem row_item() { return MxItem{static_cast<int>(threadIdx.x) >> 2, static_cast<int>(threadIdx.x) & 3}; }
+
+__device__ __forceinline__ void put_row(MxTile& t, const MxItem& it, const float (&v)[32]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 x = *reinterpret_cast<const float4*>(&t.v[tile_at(r, b * 32 + 4 * i)]);
-            v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
-        }
-        const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
-        const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&w)[4]) {
-            mx_random8(first_row + static_cast<uint32_t>(r0) + r, (random_c0 >> 3) + b * 4 + q, keys, w);
-            if constexpr (KEEP) *reinterpret_cast<uint4*>(&t.random[random_chunk(r, b * 4 + q)]) = make_uint4(w[0], w[1], w[2], w[3]);
-        });
-        if (inside) {
-            stg128(out.codes + (r0 + r) * out.code_stride + block * 16, codes);
-            out.scales[mx_scale_at(out, r0 + r, block)] = static_cast<uint8_t>(byte);
-        } else if (out.tiles && (b * 32 < width || (fill && block < (blocks + 3) / 4 * 4))) {
-            out.scales[mx_scale_at(out, r0 + r, block)] = 0;
-        }
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<float4*>(&t.v[tile_at(it.r, it.b * 32 + 4 * i)]) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+__device__ __forceinline__ void get_row(const MxTile& t, const MxItem& it, float (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float4 x = *reinterpret_cast<const float4*>(&t.v[tile_at(it.r, it.b * 32 + 4 * i)]);
+        v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
     }
 }
 
-// The same along the columns: the tile's column c becomes row q0 + c of `out`, whose blocks run over the tile's rows from r0 on.
+// The thread's row block -> codes and scale of `out`: the tile starts at row r0, column c0 (a multiple of 32) of that matrix and `height` x `width`
+// of it count.  `fill`: the tile ends the matrix on the right, and its row of scales is filled up with zeros.
+template <bool STOCHASTIC, bool KEEP>
+__device__ __forceinline__ void encode_row(MxTile& t, const MxItem& it, const float (&v)[32], const MxView& out, uint64_t r0, uint64_t c0, int height, int width, bool fill,
+                                           const RoundKeys& keys, uint32_t first_row) {
+    const uint64_t blocks = mx_blocks(out.cols), block = c0 / 32 + it.b;
+    const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
+    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&w)[4]) {
+        mx_random8(first_row + static_cast<uint32_t>(r0) + it.r, block * 4 + q, keys, w);
+        if constexpr (KEEP) *reinterpret_cast<uint4*>(&t.random[random_chunk(it.r, it.b * 4 + q)]) = make_uint4(w[0], w[1], w[2], w[3]);
+    });
+    if (it.r < height && it.b * 32 < width) {
+        stg128(out.codes + (r0 + it.r) * out.code_stride + block * 16, codes);
+        out.scales[mx_scale_at(out, r0 + it.r, block)] = static_cast<uint8_t>(byte);
+    } else if (out.tiles && (it.b * 32 < width || (fill && block < (blocks + 3) / 4 * 4))) {
+        out.scales[mx_scale_at(out, r0 + it.r, block)] = 0;
+    }
+}
+
+// The thread's column block: column c of the tile becomes row q0 + c of `out`, whose blocks run over the tile's rows from r0 on.
 // `fill`: the tile ends `out` below, and the rest of its last 128 rows gets zero scales.
 template <bool STOCHASTIC>
-__device__ __forceinline__ void tile_cols(const MxTile& t, const MxView& out, uint64_t q0, uint64_t r0, int height, int width, bool fill) {
-    const uint64_t blocks = mx_blocks(out.cols);
-    for (int item = threadIdx.x; item < kTile * 4; item += blockDim.x) {
-        const int c = item & (kTile - 1), b = item >> 7;
-        const uint64_t block = r0 / 32 + b, row = q0 + c;
-        float v[32];
+__device__ __forceinline__ void encode_col(const MxTile& t, const MxView& out, uint64_t q0, uint64_t r0, int height, int width, bool fill) {
+    const int c = threadIdx.x & (kTileCols - 1), b = threadIdx.x >> 7;
+    const uint64_t blocks = mx_blocks(out.cols), block = r0 / 32 + b, row = q0 + c;
+    float v[32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = t.v[tile_at(b * 32 + i, c)];
-        const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
-        const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&w)[4]) {
-            const unsigned short* random = reinterpret_cast<const unsigned short*>(t.random);
+    for (int i = 0; i < 32; ++i) v[i] = t.v[tile_at(b * 32 + i, c)];
+    const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
+    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&w)[4]) {
+        const unsigned short* random = reinterpret_cast<const unsigned short*>(t.random);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = b * 32 + q * 8 + 2 * i;
-                const uint32_t lo = random[2 * random_chunk(r, c >> 3) + (c & 7)], hi = random[2 * random_chunk(r + 1, c >> 3) + (c & 7)];
-                w[i] = lo | (hi << 16);
-            }
-        });
-        if (c < width && b * 32 < height) {
-            stg128(out.codes + row * out.code_stride + block * 16, codes);
-            out.scales[mx_scale_at(out, row, block)] = static_cast<uint8_t>(byte);
-        } else if (out.tiles && block < (blocks + 3) / 4 * 4 && (c < width || (fill && row < (out.rows + 127) / 128 * 128))) {
-            out.scales[mx_scale_at(out, row, block)] = 0;
+        for (int i = 0; i < 4; ++i) {
+            const int r = b * 32 + q * 8 + 2 * i;
+            const uint32_t lo = random[2 * random_chunk(r, c >> 3) + (c & 7)], hi = random[2 * random_chunk(r + 1, c >> 3) + (c & 7)];
+            w[i] = lo | (hi << 16);
         }
+    });
+    if (c < width && b * 32 < height) {
+        stg128(out.codes + row * out.code_stride + block * 16, codes);
+        out.scales[mx_scale_at(out, row, block)] = static_cast<uint8_t>(byte);
+    } else if (out.tiles && block < (blocks + 3) / 4 * 4 && (c < width || (fill && row < (out.rows + 127) / 128 * 128))) {
+        out.scales[mx_scale_at(out, row, block)] = 0;
     }
 }
 
-// The tile's elements from memory, zeros outside.  `wide`: 16 bytes a thread at a time, consecutive threads in consecutive places; else one
-// element, for rows on any boundary.
-template <bool BF16>
-__device__ __forceinline__ void load_tile(float* tile, const MxInput& in, uint64_t r0, uint64_t c0, int height, int width) {
-    constexpr int kSize = BF16 ? 2 : 4, kPer = 16 / kSize, kLanes = kTile / kPer;      // threads in a row
-    const char* base = static_cast<const char*>(in.data) + (r0 * in.stride + c0) * kSize;
-    if (in.wide) {
-        const int c = (threadIdx.x % kLanes) * kPer;
-#pragma unroll 8
-        for (int r = threadIdx.x / kLanes; r < kTile; r += kThreads / kLanes) {
-            float x[kPer];
-            const char* p = base + (static_cast<uint64_t>(r) * in.stride + c) * kSize;
-            if (r < height && c + kPer <= width) {
-                const uint4 w4 = ldg128(p);
-                const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if constexpr (BF16) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
-                    else x[k] = __uint_as_float(w[k]);
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) x[k] = r < height && c + k < width ? load1<BF16>(p, k) : 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < kPer; k += 4) *reinterpret_cast<float4*>(&tile[tile_at(r, c + k)]) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-        }
-    } else {
-        const int c = threadIdx.x % kTile;
-#pragma unroll 16
-        for (int r = threadIdx.x / kTile; r < kTile; r += kThreads / kTile)
-            tile[tile_at(r, c)] = r < height && c < width ? load1<BF16>(base, static_cast<uint64_t>(r) * in.stride + c) : 0.0f;
-    }
+__device__ __forceinline__ int within(uint64_t size, uint64_t from, int most) {
+    return from >= size ? 0 : size - from < static_cast<uint64_t>(most) ? static_cast<int>(size - from) : most;
 }
 
 template <bool BF16, bool STOCHASTIC, bool BOTH>
-__global__ void __launch_bounds__(kThreads) mx_tile_kernel(MxInput in, MxView out, MxView out_t, uint32_t tiles_across, RoundKeys keys, uint32_t first_row) {
+__global__ void __launch_bounds__(kThreads, 3) mx_tile_kernel(MxInput in, MxView out, MxView out_t, uint32_t tiles_across, RoundKeys keys, uint32_t first_row) {
     extern __shared__ __align__(16) unsigned char raw[];
     MxTile& t = *reinterpret_cast<MxTile*>(raw);
     pdl_wait();
-    const uint64_t r0 = static_cast<uint64_t>(blockIdx.x / tiles_across) * kTile, c0 = static_cast<uint64_t>(blockIdx.x % tiles_across) * kTile;
-    const int height = static_cast<int>(out.rows - r0 < kTile ? out.rows - r0 : kTile), width = static_cast<int>(out.cols - c0 < kTile ? out.cols - c0 : kTile);
-    load_tile<BF16>(t.v, in, r0, c0, height, width);
-    __syncthreads();
-    tile_rows<STOCHASTIC, BOTH>(t, out, r0, c0, height, width, true, keys, first_row, c0);
+    const uint64_t r0 = static_cast<uint64_t>(blockIdx.x / tiles_across) * kTileRows, c0 = static_cast<uint64_t>(blockIdx.x % tiles_across) * kTileCols;
+    const int height = within(out.rows, r0, kTileRows), width = within(out.cols, c0, kTileCols);
+    const MxItem it = row_item();
+    float v[32];
+    if (in.wide) {
+        load_row_block<BF16>(in.data, (r0 + it.r) * in.stride + c0 + it.b * 32, true, it.r < height ? width - it.b * 32 : 0, v);
+        if constexpr (BOTH) put_row(t, it, v);
+    } else {                               // rows on any boundary: one element a thread at a time, neighbours side by side
+        const int c = threadIdx.x % kTileCols;
+#pragma unroll 16
+        for (int r = threadIdx.x / kTileCols; r < kTileRows; r += kThreads / kTileCols)
+            t.v[tile_at(r, c)] = r < height && c < width ? load1<BF16>(in.data, (r0 + r) * in.stride + c0 + c) : 0.0f;
+        __syncthreads();
+        get_row(t, it, v);
+    }
+    encode_row<STOCHASTIC, BOTH>(t, it, v, out, r0, c0, height, width, true, keys, first_row);
     if constexpr (BOTH) {
-        if constexpr (STOCHASTIC) __syncthreads();
-        tile_cols<STOCHASTIC>(t, out_t, c0, r0, height, width, true);
+        __syncthreads();
+        encode_col<STOCHASTIC>(t, out_t, c0, r0, height, width, true);
     }
 }
 
@@ -275,62 +267,59 @@ __global__ void __launch_bounds__(kThreads) mx_aggregate_kernel(MxView m, float*
 }
 
 // ---- backward pass of the gated block's activation ----------------------------------------------------------------------
-// A block owns 128 tokens x 128 features and goes through it three times: dg = dh u a'(g), du = dh a(g), h = a(g) u, each made in fp32
-// in the tile and quantised from there, so that none of the three goes to memory in a wide type.
+// A block owns 64 tokens x 128 features: dg = dh u a'(g), du = dh a(g) and h = a(g) u are made in fp32 in registers and go through the
+// tile one after another, so that none of the three goes to memory in a wide type.
 struct MxGatedInput {
     const void* dh;
     const void* gu;                // [tokens][>= 2 features]: g, then u
     uint64_t dh_stride, gu_stride, features;
+    uint32_t wide;                 // 1: all rows start on 16-byte boundaries
 };
-template <bool BF16, bool GELU, int PART>
-__device__ __forceinline__ void gated_tile(float* tile, const MxGatedInput& in, uint64_t r0, uint64_t c0, int height, int width) {
-    const int c = threadIdx.x % kTile;
-#pragma unroll 8
-    for (int r = threadIdx.x / kTile; r < kTile; r += kThreads / kTile) {
-        float x = 0.0f;
-        if (r < height && c < width) {
-            const uint64_t at = (r0 + r) * in.gu_stride + c0 + c;
-            const float g = load1<BF16>(in.gu, at);
-            float a, da;
-            gate_value_slope<GELU>(g, a, da);
-            if constexpr (PART == 2) x = a * load1<BF16>(in.gu, at + in.features);
-            else {
-                const float dh = load1<BF16>(in.dh, (r0 + r) * in.dh_stride + c0 + c);
-                x = PART == 1 ? dh * a : dh * load1<BF16>(in.gu, at + in.features) * da;
-            }
-        }
-        tile[tile_at(r, c)] = x;
-    }
-}
 template <bool BF16, bool GELU, bool STOCHASTIC>
-__global__ void __launch_bounds__(kThreads) mx_gated_backward_kernel(MxGatedInput in, MxView dgu, MxView dgu_t, MxView h_t, uint32_t tiles_across, RoundKeys keys) {
+__global__ void __launch_bounds__(kThreads, 2) mx_gated_backward_kernel(MxGatedInput in, MxView dgu, MxView dgu_t, MxView h_t, uint32_t tiles_across, RoundKeys keys) {
     extern __shared__ __align__(16) unsigned char raw[];
     MxTile& t = *reinterpret_cast<MxTile*>(raw);
     pdl_wait();
-    const uint64_t r0 = static_cast<uint64_t>(blockIdx.x / tiles_across) * kTile, c0 = static_cast<uint64_t>(blockIdx.x % tiles_across) * kTile;
-    const int height = static_cast<int>(dgu.rows - r0 < kTile ? dgu.rows - r0 : kTile);
-    const int width = static_cast<int>(in.features - c0 < kTile ? in.features - c0 : kTile);
-    const bool last = c0 + kTile >= in.features;
+    const uint64_t r0 = static_cast<uint64_t>(blockIdx.x / tiles_across) * kTileRows, c0 = static_cast<uint64_t>(blockIdx.x % tiles_across) * kTileCols;
+    const int height = within(dgu.rows, r0, kTileRows), width = within(in.features, c0, kTileCols);
+    const bool last = c0 + kTileCols >= in.features;
+    const MxItem it = row_item();
+    const int count = it.r < height ? width - it.b * 32 : 0;
+    const uint64_t row = r0 + it.r, col = c0 + it.b * 32;
+    float dh[32], g[32], u[32];                // become dh, the value and the slope of the activation, and what is made of them
+    load_row_block<BF16>(in.dh, row * in.dh_stride + col, in.wide, count, dh);
+    load_row_block<BF16>(in.gu, row * in.gu_stride + col, in.wide, count, g);
+    load_row_block<BF16>(in.gu, row * in.gu_stride + in.features + col, in.wide, count, u);
+    float x[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        float a, slope;
+        gate_value_slope<GELU>(g[i], a, slope);
+        x[i] = dh[i] * u[i] * slope;           // dg
+        dh[i] = dh[i] * a;                     // du
+        u[i] = a * u[i];                       // h
+    }
 #pragma unroll 1
     for (int part = 0; part < 2; ++part) {
         const uint64_t at = part ? in.features + c0 : c0;
-        if (part) gated_tile<BF16, GELU, 1>(t.v, in, r0, c0, height, width);
-        else gated_tile<BF16, GELU, 0>(t.v, in, r0, c0, height, width);
+        put_row(t, it, x);
+        encode_row<STOCHASTIC, true>(t, it, x, dgu, r0, at, height, width, false, keys, 0);
         __syncthreads();
-        tile_rows<STOCHASTIC, true>(t, dgu, r0, at, height, width, false, keys, 0, at);
-        if constexpr (STOCHASTIC) __syncthreads();
-        tile_cols<STOCHASTIC>(t, dgu_t, at, r0, height, width, false);
+        encode_col<STOCHASTIC>(t, dgu_t, at, r0, height, width, false);
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) { x[i] = dh[i]; }
     }
     // [dg | du] ends anywhere in its last scale tiles, since du starts behind dg: fill them up from there
     if (last && dgu.tiles)
-        for (uint64_t block = mx_blocks(dgu.cols) + threadIdx.x / kTile; block < (mx_blocks(dgu.cols) + 3) / 4 * 4; block += kThreads / kTile)
-             dgu.scales[mx_scale_at(dgu, r0 + threadIdx.x % kTile, block)] = 0;
+        for (uint64_t block = mx_blocks(dgu.cols) + threadIdx.x / kTileRows; block < (mx_blocks(dgu.cols) + 3) / 4 * 4; block += kThreads / kTileRows)
+            dgu.scales[mx_scale_at(dgu, r0 + threadIdx.x % kTileRows, block)] = 0;
     if (last && dgu_t.tiles)
-        for (uint64_t row = dgu_t.rows + threadIdx.x / 4; row < (dgu_t.rows + 127) / 128 * 128; row += kThreads / 4) dgu_t.scales[mx_scale_at(dgu_t, row, r0 / 32 + threadIdx.x % 4)] = 0;
-    gated_tile<BF16, GELU, 2>(t.v, in, r0, c0, height, width);
+        for (uint64_t q = dgu_t.rows + threadIdx.x / 2; q < (dgu_t.rows + 127) / 128 * 128; q += kThreads / 2)
+            dgu_t.scales[mx_scale_at(dgu_t, q, r0 / 32 + threadIdx.x % 2)] = 0;
+    put_row(t, it, u);
     __syncthreads();
-    tile_cols<false>(t, h_t, c0, r0, height, width, last);
+    encode_col<false>(t, h_t, c0, r0, height, width, last);
 }
 
 template <class K>
@@ -352,7 +341,7 @@ cudaError_t launch_quantize_as(const MxQuantizeCall& c) {
         return launch_kernel(mx_rows_kernel<BF16, STOCHASTIC>, dim3(static_cast<unsigned>(across * ((rows_out + high - 1) / high))), kThreads, 0, c.stream, in, out, shift,
                              across, keys, c.first_row);
     }
-    const uint64_t across = (cols + kTile - 1) / kTile, down = (rows + kTile - 1) / kTile;
+    const uint64_t across = (cols + kTileCols - 1) / kTileCols, down = (rows + 127) / 128 * 2;       // whole scale tiles
     const dim3 grid(static_cast<unsigned>(across * down));
     if (c.out_t) {
         if (const cudaError_t e = allow_smem(mx_tile_kernel<BF16, STOCHASTIC, true>, sizeof(MxTile))) return e;
@@ -364,8 +353,10 @@ cudaError_t launch_quantize_as(const MxQuantizeCall& c) {
 
 template <bool BF16, bool GELU, bool STOCHASTIC>
 cudaError_t launch_gated_backward_as(const MxGatedBackwardCall& c) {
-    const uint64_t features = c.h_t->rows, across = (features + kTile - 1) / kTile, down = (c.dgu->rows + kTile - 1) / kTile;
-    const MxGatedInput in{c.dh, c.gu, c.dh_stride, c.gu_stride, features};
+    const uint64_t features = c.h_t->rows, across = (features + kTileCols - 1) / kTileCols, down = (c.dgu->rows + 127) / 128 * 2;
+    const uint64_t size = BF16 ? 2 : 4;
+    const MxGatedInput in{c.dh, c.gu, c.dh_stride, c.gu_stride, features,
+                          (reinterpret_cast<uintptr_t>(c.dh) | reinterpret_cast<uintptr_t>(c.gu) | (c.dgu->rows > 1 ? (c.dh_stride | c.gu_stride) * size : 0)) % 16 == 0};
     auto* kernel = mx_gated_backward_kernel<BF16, GELU, STOCHASTIC>;
     if (const cudaError_t e = allow_smem(kernel, sizeof(MxTile))) return e;
     return launch_kernel(kernel, dim3(static_cast<unsigned>(across * down)), kThreads, sizeof(MxTile), c.stream, in, mx_view(*c.dgu), mx_view(*c.dgu_t), mx_view(*c.h_t),
