@@ -1,5 +1,6 @@
 // Products of microscaled 4-bit matrices on the tensor cores: C = A B^T, and both projections of a gated feed-forward block with
-// its activation and the product of the two.
+// its activation and the product of the two.  Every wait inside a kernel is bounded: a block that gives up lets its copies and
+// multiplications end, frees its tensor memory and counts itself.
 #include <cuda.h>
 
 #include "tq_mx.cuh"
@@ -18,25 +19,53 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
 __device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
     return static_cast<uint64_t>((addr & 0x3FFFF) >> 4) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46);
 }
-// Instruction descriptor of kind::mxf4: both operands E2M1 (1) and K-major, E8M0 scales, M = 128, N; `id` = 0 or 2, the pair of bytes of the
-// scale columns that this step of 64 elements takes.
-__device__ __forceinline__ uint32_t mxf4_desc(uint32_t n, uint32_t id) {
-    return (id << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((128u >> 4) << 24) | (id << 29);
+// Instruction descriptor of kind::mxf4: both operands E2M1 (1) and K-major, E8M0 scales, M and N of the tile; `id` = 0 or 2, the pair of
+// bytes of the scale columns that this step of 64 elements takes.
+__device__ __forceinline__ uint32_t mxf4_desc(uint32_t m, uint32_t n, uint32_t id) {
+    return (id << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24) | (id << 29);
 }
+template <bool PAIR>
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {       // 128 x 4 scales -> 4 columns, in all four quarters
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+// 128 x 4 scales -> 4 columns, in all four quarters of tensor memory (of both blocks of a pair, each from its own shared memory)
+template <bool PAIR>
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+    if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
+// What was issued so far arrives on `bar` when it is done; of a pair, on both blocks' barriers
+template <bool PAIR>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(static_cast<unsigned short>(3)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_alloc(uint32_t to, uint32_t columns) {
+    if constexpr (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
 }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // 32 columns of this warp's 32 lanes: thread l gets lane l
 __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
     uint32_t r[32];
@@ -55,6 +84,23 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// The same by a block of a pair; `bar` may be the other block's.
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// ---- blocks of a cluster -----------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t of_rank(uint32_t addr, uint32_t rank) {          // the same place in another block's shared memory
+    uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank)); return r;
+}
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ float4 load_from(uint32_t cluster_addr) {
+    float4 v; asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory"); return v;
+}
 
 __device__ unsigned int g_product_wait_expired = 0;       // blocks whose bounded wait ran out, since load
 
@@ -71,200 +117,483 @@ __device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, vola
     return false;
 }
 
-// ---- the kernel for many rows ------------------------------------------------------------------------------------
-constexpr int kBM = 128, kBN = 256, kBK = 256;                   // rows of A, rows of B, elements of both in a stage
-constexpr int kStages = 4;
-constexpr uint32_t kABytes = kBM * kBK / 2, kBBytes = kBN * kBK / 2, kSABytes = kBM * kBK / 32, kSBBytes = kBN * kBK / 32;
-constexpr uint32_t kStageBytes = kABytes + kBBytes + kSABytes + kSBBytes;
-constexpr uint32_t kScaleColumns = 24;                           // of tensor memory, per stage: 2 x 4 for A, 2 x 8 for B
-constexpr uint32_t kProductSmem = kStages * kStageBytes + 1024 + 256;
-constexpr int kProductThreads = 192;
+// The same for all threads of a warp, with one answer.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* dead) { return __all_sync(0xFFFFFFFFu, wait_or_dead(bar, parity, dead)); }
+// One thread of the warp issues.  The others go through the same loops, so that descriptors, addresses and barriers stay uniform over the warp: computed
+// by the one thread alone, they are moved to uniform registers one by one for each instruction, and a multiplication took 223 clocks where 128 are needed.
+__device__ __forceinline__ bool elect() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 
 struct ProductArgs {
     const uint8_t *a_scales, *b0_scales, *b1_scales;             // in tiles
     uint64_t a_band, b0_band, b1_band;                           // bytes between 128 rows
     uint32_t m, n, k;                                            // n: columns of C, or features
     uint32_t tiles_m, tiles_n;
+    uint32_t a_rows;                                             // rows of A in a box (small kernel)
     void* out;                                                   // C, or the two projections (may be null)
     uint64_t out_stride;
-    uint32_t out_bf16, out_wide;                                 // wide: rows start on 16-byte boundaries
+    uint32_t out_bf16, out_wide;                                 // rows start on boundaries of this many bytes: 32, 16 or 0 for fewer
     MxView h;                                                    // gated only
 };
 
-// 32 consecutive elements of one row.
-__device__ __forceinline__ void store32(const ProductArgs& p, uint64_t row, uint64_t col, const float (&v)[32], uint32_t n, uint64_t offset) {
+__device__ __forceinline__ void stg256_words(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+                 :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "l"(p) : "memory");
+}
+// WIDTH consecutive elements of one row, 32 or 4 of them; columns from n on are left out.
+template <int WIDTH>
+__device__ __forceinline__ void store_row(const ProductArgs& p, uint64_t row, uint64_t col, const float (&v)[WIDTH], uint32_t n, uint64_t offset) {
+    const bool whole = col + WIDTH <= n;
     if (p.out_bf16) {
         unsigned short* to = static_cast<unsigned short*>(p.out) + row * p.out_stride + offset + col;
-        if (p.out_wide && col + 32 <= n) {
+        uint32_t w[WIDTH / 2];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                stg128(to + 8 * i, make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]), pack_bf16(v[8 * i + 4], v[8 * i + 5]),
-                                              pack_bf16(v[8 * i + 6], v[8 * i + 7])));
+        for (int i = 0; i < WIDTH / 2; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+        if (whole && p.out_wide >= 16) {
+            if constexpr (WIDTH == 4) {
+                asm volatile("st.global.v2.b32 [%0], {%1, %2};" ::"l"(to), "r"(w[0]), "r"(w[1]) : "memory");
+            } else if (p.out_wide == 32) {
+#pragma unroll
+                for (int i = 0; i < WIDTH / 16; ++i) {
+                    const uint32_t x[8] = {w[8 * i], w[8 * i + 1], w[8 * i + 2], w[8 * i + 3], w[8 * i + 4], w[8 * i + 5], w[8 * i + 6], w[8 * i + 7]};
+                    stg256_words(to + 16 * i, x);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < WIDTH / 8; ++i) stg128(to + 8 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (col + i < n) to[i] = static_cast<unsigned short>(pack_bf16(v[i], 0.0f));
+            for (int i = 0; i < WIDTH; ++i)
+                if (col + i < n) to[i] = static_cast<unsigned short>(i & 1 ? w[i / 2] >> 16 : w[i / 2]);
         }
     } else {
         float* to = static_cast<float*>(p.out) + row * p.out_stride + offset + col;
-        if (p.out_wide && col + 32 <= n) {
+        if (whole && p.out_wide >= 16) {
+            if (WIDTH >= 8 && p.out_wide == 32) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                stg128(to + 4 * i, make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+                for (int i = 0; i < WIDTH / 8; ++i) {
+                    const float x[8] = {v[8 * i], v[8 * i + 1], v[8 * i + 2], v[8 * i + 3], v[8 * i + 4], v[8 * i + 5], v[8 * i + 6], v[8 * i + 7]};
+                    stg256(to + 8 * i, x);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < WIDTH / 4; ++i)
+                    stg128(to + 4 * i, make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
+            for (int i = 0; i < WIDTH; ++i)
                 if (col + i < n) to[i] = v[i];
         }
     }
 }
+// One block of h from both projections: stores what is kept of them and the codes, returns the scale byte.
+template <bool GELU>
+__device__ __forceinline__ uint32_t store_gated(const ProductArgs& p, uint64_t row, uint64_t f, const float (&g)[32], const float (&u)[32]) {
+    if (p.out) {
+        store_row<32>(p, row, f, g, p.n, 0);
+        store_row<32>(p, row, f, u, p.n, p.n);
+    }
+    float h[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) h[i] = gate_value<GELU>(g[i]) * u[i];
+    const uint32_t byte = mx_scale_byte<false>(max_abs_32(h));
+    stg128(p.h.codes + row * p.h.code_stride + f / 2, mx_encode32<false>(h, byte, [](int, uint32_t (&)[4]) {}));
+    return byte;
+}
 
-// GATED: 0 a plain product, 1 SiLU, 2 GELU.  One block an SM, over the tiles of the result in turn.  Warp 0 loads, warp 1 multiplies, warps 2 to 5
-// take the result out of tensor memory.
+// The scale tiles of the operands as rows of words (pair kernel: bulk copies without a map count on their own block's barriers alone).
+struct ScaleMaps {
+    CUtensorMap a, b0, b1;
+};
+
+constexpr int kBK = 256;                                         // elements of both operands in a stage: 128 bytes a row
+
+// ---- large results ------------------------------------------------------------------------------------------------
+// Two blocks on neighbouring SMs make a 256 x 256 tile with one stream of multiplications: each holds 128 rows of A, half of the 256 rows
+// of B and 128 rows of the result, so that a stage of 32 KB of codes feeds 4 multiplications of 256 x 256 x 64 (512 clocks at the
+// nominal rate).  GATED: the first block holds rows of w_gate and the second the same rows of w_up; the result's columns 0 .. 127
+// are g and 128 .. 255 u of the same features.
+// Warp 0 of each block loads, and the bytes count on the first block's barrier; its warp 1 multiplies; warps 2 to 9 of both take results out of
+// tensor memory, two of them for each quarter of its lanes.  (A message from block to block for every stage, with the ordering of a release over the
+// cluster, took 0.8 us a stage: 8192 x 4096 x 16384 in 375 us.)
+// Tensor memory: two accumulators of 256 columns that overlap in the middle, at 0 and 112, and the scales of 6 stages from 368 on.  The
+// columns that both use are taken out first, and the next tile begins when they are.
+constexpr int kPairStages = 6, kPairThreads = 320;
+constexpr uint32_t kPairCodes = 2 * 128 * kBK / 2, kPairStage = kPairCodes + 3 * 1024;       // A, B; scales of 128 rows of A and of 256 rows of B
+constexpr uint32_t kPairSmem = kPairStages * kPairStage + 1024 + 256;
+constexpr uint32_t kSecond = 112, kPairScales = kSecond + 256, kPairScaleColumns = 24;
+static_assert(kPairScales + kPairStages * kPairScaleColumns == 512, "tensor memory has 512 columns");
+
+// GATED: 0 a plain product, 1 SiLU, 2 GELU.
 template <int GATED>
-__global__ void __launch_bounds__(kProductThreads, 1) mx_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0,
-                                                                        const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ ProductArgs p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0,
+                                                                                          const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ ScaleMaps maps,
+                                                                                          const __grid_constant__ ProductArgs p) {
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
     __shared__ uint32_t tmem_base;
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
-    const uint32_t bars = base + kStages * kStageBytes;
+    const uint32_t bars = base + kPairStages * kPairStage;
+    const auto full = [&](int s) { return bars + 8 * s; };                           // first block: the loads of both
+    const auto empty = [&](int s) { return bars + 8 * (kPairStages + s); };          // the multiplications have read the stage
+    const uint32_t done = bars + 8 * (2 * kPairStages), drained = done + 8, flushed = done + 16;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = cluster_rank();
+    if (threadIdx.x == 0) {
+        dead = 0;
+        for (int s = 0; s < kPairStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        mbar_init(done, 1); mbar_init(drained, 16); mbar_init(flushed, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    if (warp == 1) tmem_alloc<true>(smem_addr(&tmem_base), 512);
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+    pdl_wait();
+    const uint32_t tmem = tmem_base;
+    const uint32_t tiles = p.tiles_m * p.tiles_n, chunks = (p.k + kBK - 1) / kBK, clusters = gridDim.x / 2;
+    constexpr uint32_t kWide = GATED ? 128 : 256;                // columns of C, or features, in a tile
+
+    if (warp == 0) {
+        const bool leader = elect();
+        uint32_t it = 0;
+        bool ok = true;
+        for (uint32_t t = blockIdx.x / 2; t < tiles && ok; t += clusters) {
+            const uint32_t band = t % p.tiles_m * 2 + rank, n0 = t / p.tiles_m * kWide;
+            for (uint32_t c = 0; c < chunks; ++c, ++it) {
+                const int s = it % kPairStages;
+                if (!(ok = warp_wait(empty(s), ((it / kPairStages) & 1) ^ 1, &dead))) break;
+                if (leader) {
+                    const uint32_t at = base + s * kPairStage, scales = at + kPairCodes, bar = of_rank(full(s), 0);
+                    if (rank == 0) mbar_expect_tx(full(s), 2 * kPairStage);       // what lies outside the matrices arrives as zeros
+                    tma_load_pair(at, &map_a, c * (kBK / 2), band * 128, bar);
+                    tma_load_pair(at + kPairCodes / 2, GATED && rank ? &map_b1 : &map_b0, c * (kBK / 2), GATED ? n0 : n0 + rank * 128, bar);
+                    tma_load_pair(scales, &maps.a, c * 256, band, bar);
+                    tma_load_pair(scales + 1024, &maps.b0, c * 256, n0 / 128, bar);
+                    tma_load_pair(scales + 2048, GATED ? &maps.b1 : &maps.b0, c * 256, GATED ? n0 / 128 : n0 / 128 + 1, bar);
+                }
+                __syncwarp();
+            }
+        }
+        if (!ok && rank == 0 && leader)                          // nothing may still be on its way into blocks that end
+            for (uint32_t j = it > kPairStages ? it - kPairStages : 0; j < it; ++j) mbar_wait(full(j % kPairStages), (j / kPairStages) & 1);
+    } else if (warp == 1 && rank == 0) {
+        const bool leader = elect();
+        // The scales of a stage are copied behind the multiplications of the stage before: they then wait for no copy (8192 x 4096 x 16384: 290 us with
+        // copies first, 250 us so, with both issued as they were before elect()).
+        const auto copy_stage = [&](uint32_t s) {
+            const uint32_t scales = base + s * kPairStage + kPairCodes, to = tmem + kPairScales + s * kPairScaleColumns;
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j) {
+                copy_scales<true>(to + 4 * j, scale_desc(scales + 512 * j));
+                copy_scales<true>(to + 8 + 8 * j, scale_desc(scales + 1024 + 512 * j));
+                copy_scales<true>(to + 12 + 8 * j, scale_desc(scales + 2048 + 512 * j));
+            }
+        };
+        const uint32_t mine = (tiles - blockIdx.x / 2 + clusters - 1) / clusters, total = mine * chunks;
+        const uint32_t last_steps = (p.k - (chunks - 1) * kBK + 63) / 64;
+        bool ok = warp_wait(full(0), 0, &dead);
+        if (ok) {
+            fence_after();
+            if (leader) copy_stage(0);
+            __syncwarp();
+        }
+        for (uint32_t n_tile = 0, it = 0; n_tile < mine && ok; ++n_tile) {
+            if (!(ok = warp_wait(drained, (n_tile & 1) ^ 1, &dead))) break;
+            const uint32_t d = tmem + (n_tile & 1) * kSecond;
+            for (uint32_t c = 0; c < chunks; ++c, ++it) {
+                const uint32_t s = it % kPairStages, next = (it + 1) % kPairStages;
+                const bool more = it + 1 < total;
+                if (more && !(ok = warp_wait(full(next), ((it + 1) / kPairStages) & 1, &dead))) break;
+                fence_after();
+                if (leader) {
+                    const uint64_t a = operand_desc(base + s * kPairStage), b = operand_desc(base + s * kPairStage + kPairCodes / 2);
+                    const uint32_t scale_a = tmem + kPairScales + s * kPairScaleColumns, scale_b = scale_a + 8;
+                    const uint32_t steps = c + 1 < chunks ? 4 : last_steps;
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)             // 64 elements, 32 bytes, are 2 in the address field
+                        if (i < steps) mma_mxf4<true>(d, a + 2 * i, b + 2 * i, mxf4_desc(256, 256, (i & 1) * 2), scale_a + 4 * (i >> 1), scale_b + 8 * (i >> 1), (c | i) != 0);
+                    if (more) copy_stage(next);
+                    mma_commit<true>(empty(s));
+                }
+                __syncwarp();
+            }
+            if (ok && leader) mma_commit<true>(done);
+            __syncwarp();
+        }
+        if (!ok && leader) {                                     // let the multiplications that were issued come to an end
+            mma_commit<true>(flushed);
+            mbar_wait(flushed, 0);
+        }
+    } else if (warp >= 2) {
+        const uint32_t quarter = warp % 4, half = (warp - 2) / 4;
+        const uint32_t tell = of_rank(drained, 0);
+        uint32_t n_tile = 0;
+        for (uint32_t t = blockIdx.x / 2; t < tiles; t += clusters, ++n_tile) {
+            const uint32_t band = t % p.tiles_m * 2 + rank, n0 = t / p.tiles_m * kWide;
+            if (!warp_wait(done, n_tile & 1, &dead)) break;
+            fence_after();
+            const uint32_t local = quarter * 32 + lane, row = band * 128 + local;
+            const uint32_t from = tmem + (n_tile & 1) * kSecond + ((quarter * 32) << 16);
+            const auto release = [&] {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_at(tell);
+            };
+            if constexpr (!GATED) {
+                // the shared columns first: of the first accumulator its last 144, of the second its first
+#pragma unroll 1
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t j = n_tile & 1 ? 2 * i + half : 7 - (2 * i + half);
+                    float v[32];
+                    tmem_load32(from + 32 * j, v);
+                    tmem_wait_loads();
+                    if (i == 2 - half) release();
+                    const uint32_t col = n0 + 32 * j;
+                    if (row < p.m && col < p.n) store_row<32>(p, row, col, v, p.n, 0);
+                    __syncwarp();
+                }
+            } else {
+                uint32_t bytes = 0;
+#pragma unroll 1
+                for (uint32_t i = 0; i < 2; ++i) {
+                    const uint32_t j = 2 * half + i, f = n0 + 32 * j;
+                    float g[32], u[32];
+                    tmem_load32(from + 32 * j, g);
+                    tmem_load32(from + 128 + 32 * j, u);
+                    tmem_wait_loads();
+                    if (i == 1) release();
+                    if (row < p.m && f < p.n) bytes |= store_gated<GATED == 2>(p, row, f, g, u) << (8 * i);
+                    __syncwarp();
+                }
+                // every row of the 128, those behind the last token with zeros
+                if (band * 128 < p.m)
+                    asm volatile("st.global.b16 [%0], %1;" ::"l"(p.h.scales + band * p.h.scale_stride + (n0 / 128) * 512 + (local % 32) * 16 + (local / 32) * 4 + 2 * half),
+                                 "h"(static_cast<unsigned short>(bytes)) : "memory");
+            }
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    cluster_sync();                                              // nobody leaves before the other's multiplications and messages are through
+    if (threadIdx.x == 0 && dead) atomicAdd(&g_product_wait_expired, 1u);
+    fence_after();
+    if (warp == 1) tmem_free<true>(tmem, 512);
+}
+
+// ---- small results ------------------------------------------------------------------------------------------------------
+// Where there are too few 256 x 256 tiles for the GPU (single tokens, short prompts): tiles of 128 rows of A and 128 rows of B (GATED: of each of
+// the two matrices), one for a cluster of S blocks that share its columns k.  Each block multiplies its part, leaves the fp32 sums in shared
+// memory, and adds up, in the order of the blocks, a slice of the columns from all of them.
+constexpr int kSmallThreads = 192;
+template <int GATED>
+struct SmallShape {
+    static constexpr int kStages = GATED ? 4 : 6;
+    static constexpr uint32_t kN = GATED ? 256 : 128;
+    static constexpr uint32_t kCodesA = 128 * kBK / 2, kCodesB = kN * kBK / 2;
+    static constexpr uint32_t kStage = kCodesA + kCodesB + 1024 + (GATED ? 2048 : 1024);
+    static constexpr uint32_t kScales = kN, kScaleColumns = 8 + kN / 16;          // columns of tensor memory
+    static constexpr uint32_t kColumns = GATED ? 512 : 256;
+    static constexpr uint32_t kPitch = kN * 4 + 16;                               // bytes of a row of partial sums
+    static constexpr uint32_t kSmem = kStages * kStage + 1024 + 256;
+    static_assert(kScales + kStages * kScaleColumns <= kColumns && 128 * kPitch <= kStages * kStage, "");
+};
+
+template <int GATED>
+__global__ void __launch_bounds__(kSmallThreads, 1) mx_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0,
+                                                                    const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ ProductArgs p, uint32_t split) {
+    using S = SmallShape<GATED>;
+    extern __shared__ unsigned char raw[];
+    __shared__ volatile int dead;
+    __shared__ uint32_t tmem_base;
+    const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t bars = base + S::kStages * S::kStage;
     const auto full = [&](int s) { return bars + 8 * s; };
-    const auto empty = [&](int s) { return bars + 8 * (kStages + s); };
-    const uint32_t done = bars + 8 * (2 * kStages), drained = done + 8, flushed = done + 16;
+    const auto empty = [&](int s) { return bars + 8 * (S::kStages + s); };
+    const uint32_t done = bars + 8 * (2 * S::kStages), flushed = done + 8;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         dead = 0;
-        for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        mbar_init(done, 1); mbar_init(drained, 4); mbar_init(flushed, 1);
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        mbar_init(done, 1); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_base)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    __syncwarp();
+    if (warp == 1) tmem_alloc<false>(smem_addr(&tmem_base), S::kColumns);
     fence_before();
     __syncthreads();
     fence_after();
     pdl_wait();
     const uint32_t tmem = tmem_base;
-    const uint32_t tiles = p.tiles_m * p.tiles_n, chunks = (p.k + kBK - 1) / kBK;
-    const uint32_t per_tile_n = GATED ? 128 : kBN;
+    const uint32_t tile = blockIdx.x / split, rank = blockIdx.x % split;
+    const uint32_t tm = tile % p.tiles_m, n0 = tile / p.tiles_m * 128;
+    const uint32_t chunks = (p.k + kBK - 1) / kBK;
+    const uint32_t first = chunks * rank / split, last = chunks * (rank + 1) / split;       // at least one: split <= chunks
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        const bool leader = elect();
         uint32_t it = 0;
-        for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-            const uint32_t tm = t % p.tiles_m, tn = t / p.tiles_m;
-            const uint32_t n0 = tn * per_tile_n;
-            for (uint32_t c = 0; c < chunks; ++c, ++it) {
-                const int s = it % kStages;
-                if (!wait_or_dead(empty(s), ((it / kStages) & 1) ^ 1, &dead)) goto loaded;
-                const uint32_t at = base + s * kStageBytes;
-                const uint32_t tiles_k = ((p.k + 127) / 128 - 2 * c) < 2 ? 1 : 2;
-                const bool second = GATED || n0 + 128 < p.n;
-                mbar_expect_tx(full(s), kABytes + kBBytes + tiles_k * 512 * (second ? 3 : 2));
-                tma_load(at, &map_a, c * (kBK / 2), tm * kBM, full(s));
-                tma_load(at + kABytes, &map_b0, c * (kBK / 2), n0, full(s));
-                tma_load(at + kABytes + kBBytes / 2, GATED ? &map_b1 : &map_b0, c * (kBK / 2), GATED ? n0 : n0 + 128, full(s));
-                const uint32_t sa = at + kABytes + kBBytes;
-                bulk_load(sa, p.a_scales + tm * p.a_band + c * 1024, tiles_k * 512, full(s));
-                bulk_load(sa + kSABytes, p.b0_scales + (n0 / 128) * p.b0_band + c * 1024, tiles_k * 512, full(s));
-                if (second)
-                    bulk_load(sa + kSABytes + 1024, GATED ? p.b1_scales + (n0 / 128) * p.b1_band + c * 1024 : p.b0_scales + (n0 / 128 + 1) * p.b0_band + c * 1024,
-                              tiles_k * 512, full(s));
+        bool ok = true;
+        for (uint32_t c = first; c < last; ++c, ++it) {
+            const int s = it % S::kStages;
+            if (!(ok = warp_wait(empty(s), ((it / S::kStages) & 1) ^ 1, &dead))) break;
+            if (leader) {
+                const uint32_t at = base + s * S::kStage, scales = at + S::kCodesA + S::kCodesB;
+                const uint32_t bytes = (p.k + 127) / 128 - 2 * c < 2 ? 512 : 1024;
+                mbar_expect_tx(full(s), p.a_rows * 128 + S::kCodesB + bytes * (GATED ? 3 : 2));
+                tma_load(at + S::kCodesA, &map_b0, c * (kBK / 2), n0, full(s));
+                if constexpr (GATED != 0) tma_load(at + S::kCodesA + S::kCodesB / 2, &map_b1, c * (kBK / 2), n0, full(s));
+                tma_load(at, &map_a, c * (kBK / 2), tm * 128, full(s));
+                bulk_load(scales, p.a_scales + tm * p.a_band + c * 1024, bytes, full(s));
+                bulk_load(scales + 1024, p.b0_scales + (n0 / 128) * p.b0_band + c * 1024, bytes, full(s));
+                if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024, bytes, full(s));
+            }
+            __syncwarp();
+        }
+        if (!ok && leader)                                       // nothing may still be on its way into a block that ends
+            for (uint32_t j = it > S::kStages ? it - S::kStages : 0; j < it; ++j) mbar_wait(full(j % S::kStages), (j / S::kStages) & 1);
+    } else if (warp == 1) {
+        const bool leader = elect();
+        const uint32_t n = GATED ? 256 : p.n - n0 < 128 ? (p.n - n0 + 15) / 16 * 16 : 128;
+        const uint32_t last_steps = (p.k - (chunks - 1) * kBK + 63) / 64;
+        uint32_t it = 0;
+        bool ok = true;
+        for (uint32_t c = first; c < last; ++c, ++it) {
+            const int s = it % S::kStages;
+            if (!(ok = warp_wait(full(s), (it / S::kStages) & 1, &dead))) break;
+            fence_after();
+            if (leader) {
+                const uint32_t at = base + s * S::kStage, scales = at + S::kCodesA + S::kCodesB;
+                const uint32_t scale_a = tmem + S::kScales + s * S::kScaleColumns, scale_b = scale_a + 8;
+                const uint32_t steps = c + 1 < chunks ? 4 : last_steps;
+                const uint64_t a = operand_desc(at), b = operand_desc(at + S::kCodesA);
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j)
+                    if (2 * j < steps) {
+                        copy_scales<false>(scale_a + 4 * j, scale_desc(scales + 512 * j));
+                        copy_scales<false>(scale_b + S::kN / 32 * j, scale_desc(scales + 1024 + 512 * j));
+                        if constexpr (GATED != 0) copy_scales<false>(scale_b + 8 * j + 4, scale_desc(scales + 2048 + 512 * j));
+                    }
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    if (i < steps) mma_mxf4<false>(tmem, a + 2 * i, b + 2 * i, mxf4_desc(128, n, (i & 1) * 2), scale_a + 4 * (i >> 1), scale_b + S::kN / 32 * (i >> 1), (it | i) != 0);
+                mma_commit<false>(empty(s));
+            }
+            __syncwarp();
+        }
+        if (leader) {
+            if (ok) mma_commit<false>(done);
+            else {                                               // let the multiplications that were issued come to an end
+                mma_commit<false>(flushed);
+                mbar_wait(flushed, 0);
             }
         }
-    loaded:
-        if (dead)                                                // nothing may still be on its way into a block that ends
-            for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j) mbar_wait(full(j % kStages), (j / kStages) & 1);
-    } else if (warp == 1 && lane == 0) {
-        uint32_t it = 0, n_tile = 0;
-        for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x, ++n_tile) {
-            const uint32_t n0 = t / p.tiles_m * per_tile_n;
-            const uint32_t n = GATED ? 256 : p.n - n0 < 256 ? (p.n - n0 + 15) / 16 * 16 : 256;
-            if (!wait_or_dead(drained, (n_tile & 1) ^ 1, &dead)) break;
-            fence_after();
-            bool ok = true;
-            for (uint32_t c = 0; c < chunks; ++c, ++it) {
-                const int s = it % kStages;
-                if (!wait_or_dead(full(s), (it / kStages) & 1, &dead)) { ok = false; break; }
-                fence_after();
-                const uint32_t at = base + s * kStageBytes, sa = at + kABytes + kBBytes;
-                const uint32_t scale_a = tmem + 256 + s * kScaleColumns, scale_b = scale_a + 8;
-                const uint32_t left = p.k - c * kBK, steps = left >= kBK ? 4 : (left + 63) / 64;
-                for (uint32_t j = 0; 2 * j < steps; ++j) {
-                    copy_scales(scale_a + 4 * j, scale_desc(sa + 512 * j));
-                    copy_scales(scale_b + 8 * j, scale_desc(sa + kSABytes + 512 * j));
-                    copy_scales(scale_b + 8 * j + 4, scale_desc(sa + kSABytes + 1024 + 512 * j));
-                }
-                for (uint32_t i = 0; i < steps; ++i)
-                    mma_mxf4(tmem, operand_desc(at + 32 * i), operand_desc(at + kABytes + 32 * i), mxf4_desc(n, (i & 1) * 2), scale_a + 4 * (i >> 1), scale_b + 8 * (i >> 1),
-                             (c | i) != 0);
-                mma_commit(empty(s));
-            }
-            if (!ok) break;
-            mma_commit(done);
-        }
-        if (dead) {                                              // let the multiplications that were issued come to an end
-            mma_commit(flushed);
-            mbar_wait(flushed, 0);
-        }
-    } else if (warp >= 2) {
-        const int quarter = warp % 4;
-        uint32_t n_tile = 0;
-        for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x, ++n_tile) {
-            const uint32_t tm = t % p.tiles_m, tn = t / p.tiles_m;
-            if (!__all_sync(0xFFFFFFFFu, wait_or_dead(done, n_tile & 1, &dead))) break;
-            fence_after();
-            const uint32_t local = quarter * 32 + lane, row = tm * kBM + local;
-            const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+        __syncwarp();
+    }
+    const uint32_t quarter = warp % 4, local = quarter * 32 + lane, row = tm * 128 + local;
+    const uint32_t from = tmem + ((quarter * 32) << 16);
+    bool fine = true;
+    if (warp >= 2) {
+        fine = warp_wait(done, 0, &dead);
+        fence_after();
+    }
+    if (split == 1) {
+        if (warp >= 2 && fine) {
             if constexpr (!GATED) {
 #pragma unroll 1
-                for (uint32_t j = 0; j < 8; ++j) {
-                    const uint32_t col = tn * kBN + 32 * j;
+                for (uint32_t j = 0; j < 4; ++j) {
+                    const uint32_t col = n0 + 32 * j;
                     if (col >= p.n) break;
                     float v[32];
-                    __syncwarp();
                     tmem_load32(from + 32 * j, v);
                     tmem_wait_loads();
-                    if (row < p.m) store32(p, row, col, v, p.n, 0);
+                    if (row < p.m) store_row<32>(p, row, col, v, p.n, 0);
+                    __syncwarp();
                 }
             } else {
-                uint32_t scales = 0;
-                const uint32_t f0 = tn * 128;
+                uint32_t bytes = 0;
 #pragma unroll 1
                 for (uint32_t j = 0; j < 4; ++j) {
                     float g[32], u[32];
-                    __syncwarp();
                     tmem_load32(from + 32 * j, g);
                     tmem_load32(from + 128 + 32 * j, u);
                     tmem_wait_loads();
-                    const uint32_t f = f0 + 32 * j;
-                    if (f < p.n && row < p.m) {
-                        if (p.out) {
-                            store32(p, row, f, g, p.n, 0);
-                            store32(p, row, f, u, p.n, p.n);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) g[i] = gate_value<GATED == 2>(g[i]) * u[i];
-                        const uint32_t byte = mx_scale_byte<false>(max_abs_32(g));
-                        stg128(p.h.codes + row * p.h.code_stride + f / 2, mx_encode32<false>(g, byte, [](int, uint32_t (&)[4]) {}));
-                        scales |= byte << (8 * j);
-                    }
+                    const uint32_t f = n0 + 32 * j;
+                    if (f < p.n && row < p.m) bytes |= store_gated<GATED == 2>(p, row, f, g, u) << (8 * j);
+                    __syncwarp();
                 }
                 // every row of the 128, those behind the last token with zeros
-                asm volatile("st.global.b32 [%0], %1;" ::"l"(p.h.scales + tm * p.h.scale_stride + tn * 512 + (local % 32) * 16 + (local / 32) * 4), "r"(scales) : "memory");
+                asm volatile("st.global.b32 [%0], %1;" ::"l"(p.h.scales + tm * p.h.scale_stride + (n0 / 128) * 512 + (local % 32) * 16 + (local / 32) * 4), "r"(bytes) : "memory");
             }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(drained);
         }
+    } else {
+        const uint32_t rows = p.m - tm * 128 < 128 ? p.m - tm * 128 : 128;
+        // the stages are free: every load has been multiplied and every multiplication is done
+        if (warp >= 2 && fine && quarter * 32 < rows) {
+#pragma unroll 1
+            for (uint32_t j = 0; j < S::kN / 32; ++j) {
+                float v[32];
+                tmem_load32(from + 32 * j, v);
+                tmem_wait_loads();
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + local * S::kPitch + 128 * j + 16 * i), "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]),
+                                 "f"(v[4 * i + 3]) : "memory");
+            }
+        }
+        __syncthreads();
+        cluster_sync();
+        if constexpr (!GATED) {
+            const uint32_t quads = 32 / split;                   // of 4 columns, in this block's slice
+            for (uint32_t item = threadIdx.x; item < rows * quads; item += kSmallThreads) {
+                const uint32_t r = item / quads, q = rank * quads + item % quads, col = n0 + 4 * q;
+                if (col >= p.n) continue;
+                float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (uint32_t b = 0; b < split; ++b) {
+                    const float4 x = load_from(of_rank(base + r * S::kPitch + 16 * q, b));
+                    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+                }
+                store_row<4>(p, tm * 128 + r, col, v, p.n, 0);
+            }
+        } else {
+            const uint32_t blocks = 4 / split;                   // of 32 features, in this block's slice: split is 2 or 4
+            for (uint32_t item = threadIdx.x; item < 128 * blocks; item += kSmallThreads) {
+                const uint32_t r = item / blocks, j = rank * blocks + item % blocks, f = n0 + 32 * j;
+                uint32_t byte = 0;
+                if (r < rows && f < p.n) {
+                    float g[32], u[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) g[i] = u[i] = 0.0f;
+                    for (uint32_t b = 0; b < split; ++b) {
+                        const uint32_t at = of_rank(base + r * S::kPitch + 128 * j, b);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 x = load_from(at + 16 * i), y = load_from(at + 512 + 16 * i);
+                            g[4 * i] += x.x; g[4 * i + 1] += x.y; g[4 * i + 2] += x.z; g[4 * i + 3] += x.w;
+                            u[4 * i] += y.x; u[4 * i + 1] += y.y; u[4 * i + 2] += y.z; u[4 * i + 3] += y.w;
+                        }
+                    }
+                    byte = store_gated<GATED == 2>(p, tm * 128 + r, f, g, u);
+                }
+                p.h.scales[tm * p.h.scale_stride + (n0 / 128) * 512 + (r % 32) * 16 + (r / 32) * 4 + j] = static_cast<uint8_t>(byte);
+            }
+        }
+        __syncthreads();
+        cluster_sync();                                          // nobody leaves while another reads its sums
     }
     __syncwarp();
+    fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && dead) atomicAdd(&g_product_wait_expired, 1u);
     fence_after();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == 1) tmem_free<false>(tmem, S::kColumns);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -291,12 +620,81 @@ cudaError_t codes_map(CUtensorMap* map, const tq_mx_t& m, uint32_t rows) {
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// Which kernel, and how many blocks share a tile.  Clocks as measured with all SMs busy: a stage of a pair takes 512, of a split block 500 (two B
+// matrices: 750) since its loads are twice as many for each multiplication; a tile's start and end cost some thousands beside them.
+struct ProductPlan {
+    bool pair;
+    uint32_t split;
+};
+ProductPlan plan_product(uint64_t m, uint64_t n, uint64_t k, bool gated) {
+    const uint64_t sms = static_cast<uint64_t>(sm_count()), chunks = (k + kBK - 1) / kBK;
+    const uint64_t wide = (m + 255) / 256 * ((n + (gated ? 127 : 255)) / (gated ? 128 : 256)), pairs = sms / 2;
+    uint64_t best = 5000 + (wide + pairs - 1) / pairs * (chunks * 512 + 700);
+    ProductPlan plan{true, 1};
+    const uint64_t narrow = (m + 127) / 128 * ((n + 127) / 128);
+    for (uint32_t split = 1; split <= (gated ? 4u : 8u) && split <= chunks; split *= 2) {
+        const uint64_t cost = 3000 + (narrow * split + sms - 1) / sms * ((chunks + split - 1) / split * (gated ? 750 : 500) + 3000 + (split > 1 ? 1500 : 0));
+        if (cost < best) { best = cost; plan = ProductPlan{false, split}; }
+    }
+    return plan;
+}
+
+template <class K>
+cudaError_t launch_clustered(K* kernel, unsigned blocks, unsigned cluster, unsigned threads, size_t smem, cudaStream_t stream, void** args) {
+    if (const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))) return e;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = cluster ? 2 : 1;
+    return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kernel), args);
+}
+
+// Scale tiles, two at a time.
+cudaError_t scales_map(CUtensorMap* map, const tq_mx_t& m) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t size[2] = {(m.cols + 127) / 128 * 128, (m.rows + 127) / 128}, stride[1] = {m.scale_stride};
+    const cuuint32_t box[2] = {256, 1}, step[2] = {1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, m.scales, size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <int GATED>
-cudaError_t launch_product_as(const CUtensorMap& a, const CUtensorMap& b0, const CUtensorMap& b1, const ProductArgs& p, cudaStream_t stream) {
-    auto* kernel = mx_product_kernel<GATED>;
-    if (const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem)) return e;
-    const uint32_t tiles = p.tiles_m * p.tiles_n, sms = static_cast<uint32_t>(sm_count());
-    return launch_kernel(kernel, dim3(tiles < sms ? tiles : sms), kProductThreads, kProductSmem, stream, a, b0, b1, p);
+cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t& b1, ProductArgs p, cudaStream_t stream) {
+    p.a_scales = a.scales; p.a_band = a.scale_stride;
+    p.b0_scales = b0.scales; p.b0_band = b0.scale_stride;
+    p.b1_scales = b1.scales; p.b1_band = b1.scale_stride;
+    p.m = static_cast<uint32_t>(a.rows); p.n = static_cast<uint32_t>(b0.rows); p.k = static_cast<uint32_t>(a.cols);
+    const uint64_t at = reinterpret_cast<uintptr_t>(p.out) | (p.m > 1 ? p.out_stride * (p.out_bf16 ? 2 : 4) : 0) | (GATED ? p.n * (p.out_bf16 ? 2 : 4) : 0);
+    p.out_wide = at % 32 == 0 ? 32 : at % 16 == 0 ? 16 : 0;
+    const ProductPlan plan = plan_product(p.m, p.n, p.k, GATED != 0);
+    p.a_rows = plan.pair || p.m >= 128 ? 128 : (p.m + 7) / 8 * 8;
+    CUtensorMap map_a, map_b0, map_b1;
+    if (const cudaError_t e = codes_map(&map_a, a, p.a_rows)) return e;
+    if (const cudaError_t e = codes_map(&map_b0, b0, 128)) return e;
+    if (GATED) {
+        if (const cudaError_t e = codes_map(&map_b1, b1, 128)) return e;
+    } else {
+        map_b1 = map_b0;
+    }
+    if (plan.pair) {
+        p.tiles_m = (p.m + 255) / 256; p.tiles_n = (p.n + (GATED ? 127 : 255)) / (GATED ? 128 : 256);
+        const uint32_t tiles = p.tiles_m * p.tiles_n, pairs = static_cast<uint32_t>(sm_count()) / 2;
+        ScaleMaps maps;
+        if (const cudaError_t e = scales_map(&maps.a, a)) return e;
+        if (const cudaError_t e = scales_map(&maps.b0, b0)) return e;
+        if (const cudaError_t e = scales_map(&maps.b1, b1)) return e;
+        void* args[] = {&map_a, &map_b0, &map_b1, &maps, &p};
+        return launch_clustered(mx_pair_kernel<GATED>, 2 * (tiles < pairs ? tiles : pairs), 0, kPairThreads, kPairSmem, stream, args);
+    }
+    p.tiles_m = (p.m + 127) / 128; p.tiles_n = (p.n + 127) / 128;
+    uint32_t split = plan.split;
+    void* args[] = {&map_a, &map_b0, &map_b1, &p, &split};
+    return launch_clustered(mx_split_kernel<GATED>, p.tiles_m * p.tiles_n * split, split, kSmallThreads, SmallShape<GATED>::kSmem, stream, args);
 }
 
 }  // namespace
@@ -304,33 +702,16 @@ cudaError_t launch_product_as(const CUtensorMap& a, const CUtensorMap& b0, const
 cudaError_t read_product_wait_expired(unsigned int* count) { return cudaMemcpyFromSymbol(count, g_product_wait_expired, sizeof(unsigned int)); }
 
 cudaError_t launch_mx_product(const tq_mx_t& a, const tq_mx_t& b, void* out, bool bf16, uint64_t out_stride, cudaStream_t stream) {
-    CUtensorMap map_a, map_b;
-    if (const cudaError_t e = codes_map(&map_a, a, kBM)) return e;
-    if (const cudaError_t e = codes_map(&map_b, b, 128)) return e;
     ProductArgs p{};
-    p.a_scales = a.scales; p.a_band = a.scale_stride; p.b0_scales = b.scales; p.b0_band = b.scale_stride;
-    p.m = static_cast<uint32_t>(a.rows); p.n = static_cast<uint32_t>(b.rows); p.k = static_cast<uint32_t>(a.cols);
-    p.tiles_m = (p.m + kBM - 1) / kBM; p.tiles_n = (p.n + kBN - 1) / kBN;
     p.out = out; p.out_stride = out_stride; p.out_bf16 = bf16;
-    p.out_wide = (reinterpret_cast<uintptr_t>(out) | (p.m > 1 ? out_stride * (bf16 ? 2 : 4) : 0)) % 16 == 0;
-    return launch_product_as<0>(map_a, map_b, map_b, p, stream);
+    return launch_product_as<0>(a, b, b, p, stream);
 }
 
 cudaError_t launch_mx_gated(const MxGatedCall& c) {
-    CUtensorMap map_x, map_g, map_u;
-    if (const cudaError_t e = codes_map(&map_x, *c.x, kBM)) return e;
-    if (const cudaError_t e = codes_map(&map_g, *c.w_gate, 128)) return e;
-    if (const cudaError_t e = codes_map(&map_u, *c.w_up, 128)) return e;
     ProductArgs p{};
-    p.a_scales = c.x->scales; p.a_band = c.x->scale_stride;
-    p.b0_scales = c.w_gate->scales; p.b0_band = c.w_gate->scale_stride;
-    p.b1_scales = c.w_up->scales; p.b1_band = c.w_up->scale_stride;
-    p.m = static_cast<uint32_t>(c.x->rows); p.n = static_cast<uint32_t>(c.w_gate->rows); p.k = static_cast<uint32_t>(c.x->cols);
-    p.tiles_m = (p.m + kBM - 1) / kBM; p.tiles_n = (p.n + 127) / 128;
     p.out = c.projections; p.out_stride = c.proj_stride; p.out_bf16 = c.proj_bf16;
-    p.out_wide = (reinterpret_cast<uintptr_t>(c.projections) | (p.m > 1 ? c.proj_stride * (c.proj_bf16 ? 2 : 4) : 0)) % 16 == 0;
     p.h = mx_view(*c.h);
-    return c.gelu ? launch_product_as<2>(map_x, map_g, map_u, p, c.stream) : launch_product_as<1>(map_x, map_g, map_u, p, c.stream);
+    return c.gelu ? launch_product_as<2>(*c.x, *c.w_gate, *c.w_up, p, c.stream) : launch_product_as<1>(*c.x, *c.w_gate, *c.w_up, p, c.stream);
 }
 
 }  // namespace tq

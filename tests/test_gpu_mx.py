@@ -197,7 +197,7 @@ def sum_bound(a, b, k):
 
 
 PRODUCTS = [(1, 1, 1), (1, 64, 32), (1, 1000, 4096), (3, 7, 64), (8, 128, 96), (16, 300, 256), (17, 129, 288), (64, 257, 130), (100, 512, 500), (127, 255, 512),
-            (128, 256, 256), (129, 1, 1000), (130, 384, 2048), (256, 512, 777), (300, 700, 1056), (513, 130, 32), (1025, 1300, 384)]
+            (128, 256, 256), (129, 1, 1000), (130, 384, 2048), (256, 512, 777), (300, 700, 1056), (513, 130, 32), (1025, 1300, 384), (4096, 3000, 320), (2300, 4100, 96), (4000, 4099, 1000)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -262,7 +262,7 @@ def bracket(x, delta, m, random=None):
 
 @pytest.mark.parametrize("dtype", [None] + DTYPES)
 @pytest.mark.parametrize("act", ["silu", "gelu"])
-@pytest.mark.parametrize("tokens,d,f", [(1, 32, 32), (1, 256, 128), (2, 1000, 96), (5, 288, 352), (40, 512, 256), (128, 300, 160), (200, 640, 416), (300, 96, 1024)])
+@pytest.mark.parametrize("tokens,d,f", [(1, 32, 32), (1, 256, 128), (2, 1000, 96), (5, 288, 352), (40, 512, 256), (128, 300, 160), (200, 640, 416), (300, 96, 1024), (4000, 288, 2080), (1300, 130, 8224)])
 def test_gated(tq, tokens, d, f, act, dtype):
     rng = np.random.default_rng(tokens + d + f)
     x, wg, wu = random_mx(tq, rng, tokens, d, 1), random_mx(tq, rng, f, d, 1), random_mx(tq, rng, f, d, 1)
