@@ -66,17 +66,22 @@ __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {
 }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-// 32 columns of this warp's 32 lanes: thread l gets lane l
-__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
-    uint32_t r[32];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-                 : "r"(addr));
+// N columns of this warp's 32 lanes: thread l gets lane l
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[N]) {
+    static_assert(N == 8 || N == 16 || N == 32, "");
+    uint32_t r[N];
+    if constexpr (N == 8)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
+    if constexpr (N == 16)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
+    if constexpr (N == 32)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]) : "r"(addr));
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < N; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // A tile of a tensor map into this block's shared memory; x in bytes, a multiple of 16.
@@ -98,10 +103,6 @@ __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.a
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-__device__ __forceinline__ float4 load_from(uint32_t cluster_addr) {
-    float4 v; asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory"); return v;
-}
-
 __device__ unsigned int g_product_wait_expired = 0;       // blocks whose bounded wait ran out, since load
 
 // A bounded wait that also ends when another thread of the block has given up.
@@ -143,7 +144,7 @@ __device__ __forceinline__ void stg256_words(void* p, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
                  :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "l"(p) : "memory");
 }
-// WIDTH consecutive elements of one row, 32 or 4 of them; columns from n on are left out.
+// WIDTH consecutive elements of one row, 32, 16 or 8 of them; columns from n on are left out.
 template <int WIDTH>
 __device__ __forceinline__ void store_row(const ProductArgs& p, uint64_t row, uint64_t col, const float (&v)[WIDTH], uint32_t n, uint64_t offset) {
     const bool whole = col + WIDTH <= n;
@@ -153,9 +154,7 @@ __device__ __forceinline__ void store_row(const ProductArgs& p, uint64_t row, ui
 #pragma unroll
         for (int i = 0; i < WIDTH / 2; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
         if (whole && p.out_wide >= 16) {
-            if constexpr (WIDTH == 4) {
-                asm volatile("st.global.v2.b32 [%0], {%1, %2};" ::"l"(to), "r"(w[0]), "r"(w[1]) : "memory");
-            } else if (p.out_wide == 32) {
+            if (WIDTH >= 16 && p.out_wide == 32) {
 #pragma unroll
                 for (int i = 0; i < WIDTH / 16; ++i) {
                     const uint32_t x[8] = {w[8 * i], w[8 * i + 1], w[8 * i + 2], w[8 * i + 3], w[8 * i + 4], w[8 * i + 5], w[8 * i + 6], w[8 * i + 7]};
@@ -173,7 +172,7 @@ __device__ __forceinline__ void store_row(const ProductArgs& p, uint64_t row, ui
     } else {
         float* to = static_cast<float*>(p.out) + row * p.out_stride + offset + col;
         if (whole && p.out_wide >= 16) {
-            if (WIDTH >= 8 && p.out_wide == 32) {
+            if (p.out_wide == 32) {
 #pragma unroll
                 for (int i = 0; i < WIDTH / 8; ++i) {
                     const float x[8] = {v[8 * i], v[8 * i + 1], v[8 * i + 2], v[8 * i + 3], v[8 * i + 4], v[8 * i + 5], v[8 * i + 6], v[8 * i + 7]};
@@ -286,8 +285,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
             for (uint32_t j = it > kPairStages ? it - kPairStages : 0; j < it; ++j) mbar_wait(full(j % kPairStages), (j / kPairStages) & 1);
     } else if (warp == 1 && rank == 0) {
         const bool leader = elect();
-        // The scales of a stage are copied behind the multiplications of the stage before: they then wait for no copy (8192 x 4096 x 16384: 290 us with
-        // copies first, 250 us so, with both issued as they were before elect()).
+        // The scales of a stage are copied behind the multiplications of the stage before, so that a tile's first are in place when it begins
+        // (8192 x 8192 x 512: 36.9 us, with copies in front of their own multiplications 38.6; no difference for long k).
         const auto copy_stage = [&](uint32_t s) {
             const uint32_t scales = base + s * kPairStage + kPairCodes, to = tmem + kPairScales + s * kPairScaleColumns;
 #pragma unroll
@@ -353,7 +352,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
                 for (uint32_t i = 0; i < 4; ++i) {
                     const uint32_t j = n_tile & 1 ? 2 * i + half : 7 - (2 * i + half);
                     float v[32];
-                    tmem_load32(from + 32 * j, v);
+                    tmem_load(from + 32 * j, v);
                     tmem_wait_loads();
                     if (i == 2 - half) release();
                     const uint32_t col = n0 + 32 * j;
@@ -366,8 +365,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
                 for (uint32_t i = 0; i < 2; ++i) {
                     const uint32_t j = 2 * half + i, f = n0 + 32 * j;
                     float g[32], u[32];
-                    tmem_load32(from + 32 * j, g);
-                    tmem_load32(from + 128 + 32 * j, u);
+                    tmem_load(from + 32 * j, g);
+                    tmem_load(from + 128 + 32 * j, u);
                     tmem_wait_loads();
                     if (i == 1) release();
                     if (row < p.m && f < p.n) bytes |= store_gated<GATED == 2>(p, row, f, g, u) << (8 * i);
@@ -390,38 +389,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
 
 // ---- small results ------------------------------------------------------------------------------------------------------
 // Where there are too few 256 x 256 tiles for the GPU (single tokens, short prompts): tiles of 128 rows of A and 128 rows of B (GATED: of each of
-// the two matrices), one for a cluster of S blocks that share its columns k.  Each block multiplies its part, leaves the fp32 sums in shared
-// memory, and adds up, in the order of the blocks, a slice of the columns from all of them.
-constexpr int kSmallThreads = 192;
+// the two matrices), one for a cluster of `split` blocks that share its columns k.  A slice of the tile's columns belongs to each block.  When all have
+// multiplied, every block sends the others their slices of its fp32 sums (remote stores wait for nothing) and keeps its own in registers, and
+// each adds up its slice in the order of the blocks.
+// Of A only as many rows as there are tokens are loaded, and stages are smaller and more for it: the multiplication reads 128 rows of whatever lies
+// there, and nobody reads the rows of the result that come from it.
+constexpr int kSplitThreads = 320;
 template <int GATED>
-struct SmallShape {
-    static constexpr int kStages = GATED ? 4 : 6;
+struct SplitShape {
     static constexpr uint32_t kN = GATED ? 256 : 128;
-    static constexpr uint32_t kCodesA = 128 * kBK / 2, kCodesB = kN * kBK / 2;
-    static constexpr uint32_t kStage = kCodesA + kCodesB + 1024 + (GATED ? 2048 : 1024);
+    static constexpr uint32_t kCodesA = 128 * kBK / 2, kCodesB = kN * kBK / 2, kScaleBytes = 1024 + (GATED ? 2048 : 1024);
+    static constexpr uint32_t kMostStages = 8;
     static constexpr uint32_t kScales = kN, kScaleColumns = 8 + kN / 16;          // columns of tensor memory
     static constexpr uint32_t kColumns = GATED ? 512 : 256;
-    static constexpr uint32_t kPitch = kN * 4 + 16;                               // bytes of a row of partial sums
-    static constexpr uint32_t kSmem = kStages * kStage + 1024 + 256;
-    static_assert(kScales + kStages * kScaleColumns <= kColumns && 128 * kPitch <= kStages * kStage, "");
+    static constexpr uint32_t kMostStageSmem = 208 * 1024;
+    static_assert(kScales + kMostStages * kScaleColumns <= kColumns, "");
+    // rows of A in a box -> bytes of a stage (boxes start on 1024 bytes), stages, and the whole allocation, in which 128 rows from the last box on stay
+    __host__ __device__ static uint32_t stage(uint32_t a_rows) { return kCodesB + (a_rows * 128 + kScaleBytes + 1023) / 1024 * 1024; }
+    static uint32_t stages(uint32_t a_rows) { return kMostStageSmem / stage(a_rows) < kMostStages ? kMostStageSmem / stage(a_rows) : kMostStages; }
+};
+// What a block receives from another one: for either half of its slice (a gated block: of 32 features, g and then u), four columns after four columns,
+// 16 bytes for each row.  A warp, which holds 32 rows, then sends 512 bytes in a piece (in pieces of 16 bytes, row after row, it took 2 us more a tile).
+template <int GATED, int SPLIT>
+struct SplitSums {
+    static constexpr int kSlice = 128 / SPLIT;                                    // columns of C, or features
+    static constexpr int kWidth = GATED ? 32 : kSlice / 2;                        // of them a thread's
+    static constexpr int kHalves = kSlice / kWidth;                               // gated, four blocks: one
+    static constexpr uint32_t kRowBytes = kWidth * 4 * (GATED ? 2 : 1);
 };
 
-template <int GATED>
-__global__ void __launch_bounds__(kSmallThreads, 1) mx_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0,
-                                                                    const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ ProductArgs p, uint32_t split) {
-    using S = SmallShape<GATED>;
+// The bytes of 8 codes are in lanes 0, 8, 16 and 24: one element a thread.
+__device__ __forceinline__ uint32_t e2m1_of_warp(float y) {
+    const float v[8] = {y, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t lane = threadIdx.x & 31;
+    return __reduce_or_sync(0xFFu << (lane & 24), e2m1_nearest8(v) << (4 * (lane & 7)));
+}
+__device__ __forceinline__ float load_shared(uint32_t addr) { float v; asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory"); return v; }
+__device__ __forceinline__ float4 load_shared4(uint32_t addr) {
+    float4 v; asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory"); return v;
+}
+
+template <int GATED, int SPLIT>
+__global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0,
+                                                                    const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ ProductArgs p, uint32_t stages,
+                                                                    uint32_t stage_bytes) {
+    using S = SplitShape<GATED>;
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
     __shared__ uint32_t tmem_base;
+    __shared__ __align__(8) uint64_t barriers[2 * S::kMostStages + 2];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
-    const uint32_t bars = base + S::kStages * S::kStage;
-    const auto full = [&](int s) { return bars + 8 * s; };
-    const auto empty = [&](int s) { return bars + 8 * (S::kStages + s); };
-    const uint32_t done = bars + 8 * (2 * S::kStages), flushed = done + 8;
+    const uint32_t bars = smem_addr(barriers);
+    const auto full = [&](uint32_t s) { return bars + 8 * s; };
+    const auto empty = [&](uint32_t s) { return bars + 8 * (S::kMostStages + s); };
+    const uint32_t done = bars + 8 * (2 * S::kMostStages), flushed = done + 8;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         dead = 0;
-        for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (uint32_t s = 0; s < stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -432,61 +457,67 @@ __global__ void __launch_bounds__(kSmallThreads, 1) mx_split_kernel(const __grid
     fence_after();
     pdl_wait();
     const uint32_t tmem = tmem_base;
-    const uint32_t tile = blockIdx.x / split, rank = blockIdx.x % split;
+    const uint32_t tile = blockIdx.x / SPLIT, rank = blockIdx.x % SPLIT;
     const uint32_t tm = tile % p.tiles_m, n0 = tile / p.tiles_m * 128;
     const uint32_t chunks = (p.k + kBK - 1) / kBK;
-    const uint32_t first = chunks * rank / split, last = chunks * (rank + 1) / split;       // at least one: split <= chunks
+    const uint32_t first = chunks * rank / SPLIT, last = chunks * (rank + 1) / SPLIT;       // at least one: SPLIT <= chunks
+    const uint32_t at_a = S::kCodesB, at_scales = S::kCodesB + p.a_rows * 128;              // within a stage
 
     if (warp == 0) {
         const bool leader = elect();
-        uint32_t it = 0;
+        uint32_t s = 0, round = 0, it = 0;
         bool ok = true;
         for (uint32_t c = first; c < last; ++c, ++it) {
-            const int s = it % S::kStages;
-            if (!(ok = warp_wait(empty(s), ((it / S::kStages) & 1) ^ 1, &dead))) break;
+            if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead))) break;
             if (leader) {
-                const uint32_t at = base + s * S::kStage, scales = at + S::kCodesA + S::kCodesB;
+                const uint32_t at = base + s * stage_bytes, scales = at + at_scales;
                 const uint32_t bytes = (p.k + 127) / 128 - 2 * c < 2 ? 512 : 1024;
                 mbar_expect_tx(full(s), p.a_rows * 128 + S::kCodesB + bytes * (GATED ? 3 : 2));
-                tma_load(at + S::kCodesA, &map_b0, c * (kBK / 2), n0, full(s));
-                if constexpr (GATED != 0) tma_load(at + S::kCodesA + S::kCodesB / 2, &map_b1, c * (kBK / 2), n0, full(s));
-                tma_load(at, &map_a, c * (kBK / 2), tm * 128, full(s));
+                tma_load(at, &map_b0, c * (kBK / 2), n0, full(s));
+                if constexpr (GATED != 0) tma_load(at + S::kCodesB / 2, &map_b1, c * (kBK / 2), n0, full(s));
+                tma_load(at + at_a, &map_a, c * (kBK / 2), tm * 128, full(s));
                 bulk_load(scales, p.a_scales + tm * p.a_band + c * 1024, bytes, full(s));
                 bulk_load(scales + 1024, p.b0_scales + (n0 / 128) * p.b0_band + c * 1024, bytes, full(s));
                 if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024, bytes, full(s));
             }
             __syncwarp();
+            if (++s == stages) { s = 0; ++round; }
         }
         if (!ok && leader)                                       // nothing may still be on its way into a block that ends
-            for (uint32_t j = it > S::kStages ? it - S::kStages : 0; j < it; ++j) mbar_wait(full(j % S::kStages), (j / S::kStages) & 1);
+            for (uint32_t j = it > stages ? it - stages : 0; j < it; ++j) mbar_wait(full(j % stages), (j / stages) & 1);
+        __syncwarp();
     } else if (warp == 1) {
         const bool leader = elect();
         const uint32_t n = GATED ? 256 : p.n - n0 < 128 ? (p.n - n0 + 15) / 16 * 16 : 128;
         const uint32_t last_steps = (p.k - (chunks - 1) * kBK + 63) / 64;
-        uint32_t it = 0;
+        const auto copy_stage = [&](uint32_t s) {                // of a chunk with one tile of scales the second is whatever lies there, and no step takes it
+            const uint32_t scales = base + s * stage_bytes + at_scales, to = tmem + S::kScales + s * S::kScaleColumns;
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j) {
+                copy_scales<false>(to + 4 * j, scale_desc(scales + 512 * j));
+                copy_scales<false>(to + 8 + S::kN / 32 * j, scale_desc(scales + 1024 + 512 * j));
+                if constexpr (GATED != 0) copy_scales<false>(to + 12 + 8 * j, scale_desc(scales + 2048 + 512 * j));
+            }
+        };
         bool ok = true;
-        for (uint32_t c = first; c < last; ++c, ++it) {
-            const int s = it % S::kStages;
-            if (!(ok = warp_wait(full(s), (it / S::kStages) & 1, &dead))) break;
+        uint32_t s = 0, round = 0;
+        for (uint32_t c = first; c < last; ++c) {
+            if (!(ok = warp_wait(full(s), round & 1, &dead))) break;
             fence_after();
             if (leader) {
-                const uint32_t at = base + s * S::kStage, scales = at + S::kCodesA + S::kCodesB;
+                const uint32_t at = base + s * stage_bytes;
                 const uint32_t scale_a = tmem + S::kScales + s * S::kScaleColumns, scale_b = scale_a + 8;
                 const uint32_t steps = c + 1 < chunks ? 4 : last_steps;
-                const uint64_t a = operand_desc(at), b = operand_desc(at + S::kCodesA);
+                const uint64_t a = operand_desc(at + at_a), b = operand_desc(at);
+                copy_stage(s);
 #pragma unroll
-                for (uint32_t j = 0; j < 2; ++j)
-                    if (2 * j < steps) {
-                        copy_scales<false>(scale_a + 4 * j, scale_desc(scales + 512 * j));
-                        copy_scales<false>(scale_b + S::kN / 32 * j, scale_desc(scales + 1024 + 512 * j));
-                        if constexpr (GATED != 0) copy_scales<false>(scale_b + 8 * j + 4, scale_desc(scales + 2048 + 512 * j));
-                    }
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i)
-                    if (i < steps) mma_mxf4<false>(tmem, a + 2 * i, b + 2 * i, mxf4_desc(128, n, (i & 1) * 2), scale_a + 4 * (i >> 1), scale_b + S::kN / 32 * (i >> 1), (it | i) != 0);
+                for (uint32_t i = 0; i < 4; ++i)                 // 64 elements, 32 bytes, are 2 in the address field
+                    if (i < steps)
+                        mma_mxf4<false>(tmem, a + 2 * i, b + 2 * i, mxf4_desc(128, n, (i & 1) * 2), scale_a + 4 * (i >> 1), scale_b + S::kN / 32 * (i >> 1), (c != first) | (i != 0));
                 mma_commit<false>(empty(s));
             }
             __syncwarp();
+            if (++s == stages) { s = 0; ++round; }
         }
         if (leader) {
             if (ok) mma_commit<false>(done);
@@ -497,96 +528,139 @@ __global__ void __launch_bounds__(kSmallThreads, 1) mx_split_kernel(const __grid
         }
         __syncwarp();
     }
-    const uint32_t quarter = warp % 4, local = quarter * 32 + lane, row = tm * 128 + local;
+    // Two warps for each quarter of the lanes.
+    const uint32_t quarter = warp % 4, half = (warp - 2) / 4, local = quarter * 32 + lane, row = tm * 128 + local;
     const uint32_t from = tmem + ((quarter * 32) << 16);
+    const uint32_t rows = p.m - tm * 128 < 128 ? p.m - tm * 128 : 128;
+    const bool taker = warp >= 2 && quarter * 32 < rows;        // has rows to take out of tensor memory
     bool fine = true;
     if (warp >= 2) {
         fine = warp_wait(done, 0, &dead);
         fence_after();
     }
-    if (split == 1) {
-        if (warp >= 2 && fine) {
-            if constexpr (!GATED) {
+    if constexpr (GATED != 0) {
+        // the scales' tile is written for all 128 rows, those behind the last token with zeros
+        uint8_t* const tail = p.h.scales + tm * p.h.scale_stride + (n0 / 128) * 512;
+        for (uint32_t item = threadIdx.x; item < (128 - rows) * (4 / SPLIT); item += kSplitThreads) {
+            const uint32_t r = rows + item / (4 / SPLIT);
+            tail[(r % 32) * 16 + (r / 32) * 4 + rank * (4 / SPLIT) + item % (4 / SPLIT)] = 0;
+        }
+    }
+    const auto put_scale = [&](uint32_t r, uint32_t j, uint32_t byte) {              // of row r and block j of the tile
+        p.h.scales[tm * p.h.scale_stride + (n0 / 128) * 512 + (r % 32) * 16 + (r / 32) * 4 + j] = static_cast<uint8_t>(byte);
+    };
+    if constexpr (SPLIT == 1) {
+        if (taker && fine) {
 #pragma unroll 1
-                for (uint32_t j = 0; j < 4; ++j) {
-                    const uint32_t col = n0 + 32 * j;
-                    if (col >= p.n) break;
-                    float v[32];
-                    tmem_load32(from + 32 * j, v);
+            for (uint32_t j = half; j < 4; j += 2) {
+                const uint32_t col = n0 + 32 * j;
+                float v[32];
+                tmem_load(from + 32 * j, v);
+                if constexpr (!GATED) {
                     tmem_wait_loads();
-                    if (row < p.m) store_row<32>(p, row, col, v, p.n, 0);
-                    __syncwarp();
-                }
-            } else {
-                uint32_t bytes = 0;
-#pragma unroll 1
-                for (uint32_t j = 0; j < 4; ++j) {
-                    float g[32], u[32];
-                    tmem_load32(from + 32 * j, g);
-                    tmem_load32(from + 128 + 32 * j, u);
+                    if (row < p.m && col < p.n) store_row<32>(p, row, col, v, p.n, 0);
+                } else {
+                    float u[32];
+                    tmem_load(from + 128 + 32 * j, u);
                     tmem_wait_loads();
-                    const uint32_t f = n0 + 32 * j;
-                    if (f < p.n && row < p.m) bytes |= store_gated<GATED == 2>(p, row, f, g, u) << (8 * j);
-                    __syncwarp();
+                    if (row < p.m) put_scale(local, j, col < p.n ? store_gated<GATED == 2>(p, row, col, v, u) : 0);
                 }
-                // every row of the 128, those behind the last token with zeros
-                asm volatile("st.global.b32 [%0], %1;" ::"l"(p.h.scales + tm * p.h.scale_stride + (n0 / 128) * 512 + (local % 32) * 16 + (local / 32) * 4), "r"(bytes) : "memory");
+                __syncwarp();
             }
         }
     } else {
-        const uint32_t rows = p.m - tm * 128 < 128 ? p.m - tm * 128 : 128;
-        // the stages are free: every load has been multiplied and every multiplication is done
-        if (warp >= 2 && fine && quarter * 32 < rows) {
-#pragma unroll 1
-            for (uint32_t j = 0; j < S::kN / 32; ++j) {
-                float v[32];
-                tmem_load32(from + 32 * j, v);
-                tmem_wait_loads();
+        using Q = SplitSums<GATED, SPLIT>;
+        const uint32_t part = rows * Q::kRowBytes, quad = rows * 16;                 // bytes from one half, or four columns, to the next
+        // Few rows of a gated block: a warp makes 32 elements, a thread one of them, and its own sums go through shared memory as well.
+        const bool few = GATED && rows * Q::kHalves <= 16;
+        const auto received = [&](uint32_t b, uint32_t h, uint32_t r) { return base + (b * Q::kHalves + h) * part + r * 16; };
+        const auto send = [&](uint32_t owner, uint32_t h) {
+            float v[Q::kWidth];
+            const uint32_t to = of_rank(received(rank, h, local), owner);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + local * S::kPitch + 128 * j + 16 * i), "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]),
-                                 "f"(v[4 * i + 3]) : "memory");
+            for (int w = 0; w < (GATED ? 2 : 1); ++w) {
+                tmem_load(from + owner * Q::kSlice + h * Q::kWidth + 128 * w, v);
+                tmem_wait_loads();
+                if (local < rows)
+#pragma unroll
+                    for (int i = 0; i < Q::kWidth; i += 4)
+                        asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(to + (w * Q::kWidth + i) / 4 * quad), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3]) : "memory");
+                __syncwarp();
+            }
+        };
+        __syncthreads();
+        cluster_sync();                                          // all blocks have multiplied: the stages are free
+        if (taker && fine) {
+#pragma unroll 1
+            for (uint32_t i = 0; i < SPLIT; ++i) {
+                const uint32_t owner = (rank + 1 + i) % SPLIT;
+                if (owner == rank && !few) continue;
+                if (Q::kHalves == 2) send(owner, half);
+                else if ((i & 1) == half) send(owner, 0);
             }
         }
         __syncthreads();
         cluster_sync();
-        if constexpr (!GATED) {
-            const uint32_t quads = 32 / split;                   // of 4 columns, in this block's slice
-            for (uint32_t item = threadIdx.x; item < rows * quads; item += kSmallThreads) {
-                const uint32_t r = item / quads, q = rank * quads + item % quads, col = n0 + 4 * q;
-                if (col >= p.n) continue;
-                float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                for (uint32_t b = 0; b < split; ++b) {
-                    const float4 x = load_from(of_rank(base + r * S::kPitch + 16 * q, b));
-                    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-                }
-                store_row<4>(p, tm * 128 + r, col, v, p.n, 0);
-            }
-        } else {
-            const uint32_t blocks = 4 / split;                   // of 32 features, in this block's slice: split is 2 or 4
-            for (uint32_t item = threadIdx.x; item < 128 * blocks; item += kSmallThreads) {
-                const uint32_t r = item / blocks, j = rank * blocks + item % blocks, f = n0 + 32 * j;
+        if (few) {
+            for (uint32_t item = warp; item < rows * Q::kHalves; item += kSplitThreads / 32) {
+                const uint32_t r = item / Q::kHalves, h = item % Q::kHalves, j = rank * Q::kHalves + h, f = n0 + 32 * j;
                 uint32_t byte = 0;
-                if (r < rows && f < p.n) {
-                    float g[32], u[32];
+                if (f < p.n) {
+                    float g = 0.0f, u = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) g[i] = u[i] = 0.0f;
-                    for (uint32_t b = 0; b < split; ++b) {
-                        const uint32_t at = of_rank(base + r * S::kPitch + 128 * j, b);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 x = load_from(at + 16 * i), y = load_from(at + 512 + 16 * i);
-                            g[4 * i] += x.x; g[4 * i + 1] += x.y; g[4 * i + 2] += x.z; g[4 * i + 3] += x.w;
-                            u[4 * i] += y.x; u[4 * i + 1] += y.y; u[4 * i + 2] += y.z; u[4 * i + 3] += y.w;
+                    for (uint32_t b = 0; b < SPLIT; ++b) {
+                        const uint32_t at = received(b, h, r) + lane / 4 * quad + lane % 4 * 4;
+                        g += load_shared(at); u += load_shared(at + 8 * quad);
+                    }
+                    const uint64_t to_row = tm * 128 + r;
+                    if (p.out) {
+                        const uint64_t to = to_row * p.out_stride + f + lane;
+                        if (p.out_bf16) {
+                            static_cast<unsigned short*>(p.out)[to] = static_cast<unsigned short>(pack_bf16(g, 0.0f));
+                            static_cast<unsigned short*>(p.out)[to + p.n] = static_cast<unsigned short>(pack_bf16(u, 0.0f));
+                        } else {
+                            static_cast<float*>(p.out)[to] = g;
+                            static_cast<float*>(p.out)[to + p.n] = u;
                         }
                     }
-                    byte = store_gated<GATED == 2>(p, tm * 128 + r, f, g, u);
+                    const float x = gate_value<GATED == 2>(g) * u;
+                    // a NaN's pattern without its sign is above infinity's, and that above all others
+                    byte = mx_scale_byte<false>(__uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x) & 0x7FFFFFFFu)));
+                    const uint32_t codes = e2m1_of_warp(x * mx_inv_scale(byte));
+                    if ((lane & 7) == 0)
+                        asm volatile("st.global.b32 [%0], %1;" ::"l"(p.h.codes + to_row * p.h.code_stride + f / 2 + lane / 2), "r"(byte == 255u ? 0u : codes) : "memory");
                 }
-                p.h.scales[tm * p.h.scale_stride + (n0 / 128) * 512 + (r % 32) * 16 + (r / 32) * 4 + j] = static_cast<uint8_t>(byte);
+                if (lane == 0) put_scale(r, j, byte);
+            }
+        } else if (taker && fine && half < Q::kHalves) {
+            const uint32_t col = n0 + rank * Q::kSlice + half * Q::kWidth;
+            float v[Q::kWidth];
+            const auto add_up = [&](float (&x)[Q::kWidth], uint32_t first_quad) {        // what the own block has in x with the others', in their order
+#pragma unroll
+                for (int i = 0; i < Q::kWidth; i += 4) {
+                    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (uint32_t b = 0; b < SPLIT; ++b) {
+                        float4 y = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                        if (b != rank && local < rows) y = load_shared4(received(b, half, local) + (first_quad + i / 4) * quad);
+                        sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
+                    }
+                    x[i] = sum.x; x[i + 1] = sum.y; x[i + 2] = sum.z; x[i + 3] = sum.w;
+                }
+            };
+            tmem_load(from + rank * Q::kSlice + half * Q::kWidth, v);
+            tmem_wait_loads();
+            add_up(v, 0);
+            if constexpr (!GATED) {
+                if (row < p.m && col < p.n) store_row<Q::kWidth>(p, row, col, v, p.n, 0);
+            } else {
+                float u[32];
+                tmem_load(from + 128 + rank * Q::kSlice + half * Q::kWidth, u);
+                tmem_wait_loads();
+                add_up(u, 8);
+                if (row < p.m) put_scale(local, rank * Q::kHalves + half, col < p.n ? store_gated<GATED == 2>(p, row, col, v, u) : 0);
             }
         }
-        __syncthreads();
-        cluster_sync();                                          // nobody leaves while another reads its sums
     }
     __syncwarp();
     fence_before();
@@ -620,20 +694,50 @@ cudaError_t codes_map(CUtensorMap* map, const tq_mx_t& m, uint32_t rows) {
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-// Which kernel, and how many blocks share a tile.  Clocks as measured with all SMs busy: a stage of a pair takes 512, of a split block 500 (two B
-// matrices: 750) since its loads are twice as many for each multiplication; a tile's start and end cost some thousands beside them.
+// Memory of a split block: its stages, or what it receives.
+struct SplitMemory {
+    uint32_t stages, stage_bytes;
+    size_t bytes;
+};
+template <int GATED>
+SplitMemory split_memory(uint32_t rows, uint32_t a_rows, uint64_t chunks, uint32_t split) {
+    using S = SplitShape<GATED>;
+    SplitMemory m{S::stages(a_rows), S::stage(a_rows), 0};
+    const uint64_t most = (chunks + split - 1) / split;
+    if (m.stages > most) m.stages = static_cast<uint32_t>(most);
+    const uint32_t sums = split > 1 ? rows * 128 * 4 * (GATED ? 2 : 1) : 0;
+    const uint32_t last = S::kCodesA > m.stage_bytes - S::kCodesB ? S::kCodesA : m.stage_bytes - S::kCodesB;      // 128 rows of A from the last box on
+    const uint32_t staged = (m.stages - 1) * m.stage_bytes + S::kCodesB + last;
+    // No more blocks on an SM than its tensor memory serves at once, two plain ones, or one gated one and nothing beside it: a block that waits for
+    // columns keeps its cluster waiting, and two clusters that hold each other's columns would wait for ever.
+    const size_t least = GATED ? 160 * 1024 : 77 * 1024, need = (staged > sums ? staged : sums) + 1024;
+    m.bytes = need > least ? need : least;
+    return m;
+}
+
+// Which kernel, and how many blocks share a tile: by an estimate of the time in ns, fitted to graphs of 20 launches.  A pair takes 430 a stage and 1300 a
+// tile at least; a split block 285 (two B matrices: 340) and up to 70 more as A's rows and the busy SMs grow.  Adding up costs 1 us and 4 ns for each row and block.
+// Measured (pair / split 1 / 2 / 4 / 8): 1 x 8192 x 4096 9.9 / 7.1 / 6.0 / 5.6 / 9.7 us, 777 x 1000 x 4000 12.6 / 10.3 / 8.9 / 14 / 17,
+// 1024 x 2048 x 4096 9.9 / 8.4 / 14 / 24 / 33, 2048^3 8.2 / 11 / 23 / 30 / 59, gated 4 x 4096 x 8192 12 / 9.2 / 7.4 / 11, gated 512 x 4096 x 8192 17 / 19 / 36 / 71.
 struct ProductPlan {
     bool pair;
     uint32_t split;
 };
-ProductPlan plan_product(uint64_t m, uint64_t n, uint64_t k, bool gated) {
-    const uint64_t sms = static_cast<uint64_t>(sm_count()), chunks = (k + kBK - 1) / kBK;
-    const uint64_t wide = (m + 255) / 256 * ((n + (gated ? 127 : 255)) / (gated ? 128 : 256)), pairs = sms / 2;
-    uint64_t best = 5000 + (wide + pairs - 1) / pairs * (chunks * 512 + 700);
+template <int GATED>
+ProductPlan plan_product(uint32_t m, uint32_t n, uint32_t k, uint32_t a_rows) {
+    const uint64_t sms = static_cast<uint64_t>(sm_count()), chunks = (static_cast<uint64_t>(k) + kBK - 1) / kBK;
+    const uint64_t wide = (static_cast<uint64_t>(m) + 255) / 256 * ((static_cast<uint64_t>(n) + (GATED ? 127 : 255)) / (GATED ? 128 : 256)), pairs = sms / 2;
+    const uint64_t tile = chunks * 430 > 1300 ? chunks * 430 : 1300;
+    uint64_t best = 3500 + (wide + pairs - 1) / pairs * tile;
     ProductPlan plan{true, 1};
-    const uint64_t narrow = (m + 127) / 128 * ((n + 127) / 128);
-    for (uint32_t split = 1; split <= (gated ? 4u : 8u) && split <= chunks; split *= 2) {
-        const uint64_t cost = 3000 + (narrow * split + sms - 1) / sms * ((chunks + split - 1) / split * (gated ? 750 : 500) + 3000 + (split > 1 ? 1500 : 0));
+    const uint64_t narrow = (static_cast<uint64_t>(m) + 127) / 128 * ((static_cast<uint64_t>(n) + 127) / 128);
+    const uint32_t rows = m < 128 ? m : 128;
+    for (uint32_t split = 1; split <= (GATED ? 4u : 8u) && split <= chunks; split *= 2) {
+        const bool two = !GATED && split_memory<GATED>(rows, a_rows, chunks, split).bytes <= 112 * 1024;
+        const uint64_t room = (split == 8 ? sms * 7 / 8 : sms) * (two ? 2 : 1), blocks = narrow * split;
+        const uint64_t waves = (blocks + room - 1) / room, stage = (GATED ? 340 : 285) + rows / 5 + 70 * (blocks < sms ? blocks : sms) / sms;
+        const uint64_t sums = split == 1 ? 500 : 800 + 100 * split + 4 * rows * split;
+        const uint64_t cost = 2600 + waves * ((chunks + split - 1) / split * stage + sums) + (waves - 1) * 1500;
         if (cost < best) { best = cost; plan = ProductPlan{false, split}; }
     }
     return plan;
@@ -663,6 +767,13 @@ cudaError_t scales_map(CUtensorMap* map, const tq_mx_t& m) {
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+template <int GATED, int SPLIT>
+cudaError_t launch_split_as(const CUtensorMap& map_a, const CUtensorMap& map_b0, const CUtensorMap& map_b1, const ProductArgs& p, cudaStream_t stream) {
+    SplitMemory mem = split_memory<GATED>(p.m < 128 ? p.m : 128, p.a_rows, (static_cast<uint64_t>(p.k) + kBK - 1) / kBK, SPLIT);
+    void* args[] = {const_cast<CUtensorMap*>(&map_a), const_cast<CUtensorMap*>(&map_b0), const_cast<CUtensorMap*>(&map_b1), const_cast<ProductArgs*>(&p), &mem.stages, &mem.stage_bytes};
+    return launch_clustered(mx_split_kernel<GATED, SPLIT>, p.tiles_m * p.tiles_n * SPLIT, SPLIT, kSplitThreads, mem.bytes, stream, args);
+}
+
 template <int GATED>
 cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t& b1, ProductArgs p, cudaStream_t stream) {
     p.a_scales = a.scales; p.a_band = a.scale_stride;
@@ -671,8 +782,9 @@ cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t
     p.m = static_cast<uint32_t>(a.rows); p.n = static_cast<uint32_t>(b0.rows); p.k = static_cast<uint32_t>(a.cols);
     const uint64_t at = reinterpret_cast<uintptr_t>(p.out) | (p.m > 1 ? p.out_stride * (p.out_bf16 ? 2 : 4) : 0) | (GATED ? p.n * (p.out_bf16 ? 2 : 4) : 0);
     p.out_wide = at % 32 == 0 ? 32 : at % 16 == 0 ? 16 : 0;
-    const ProductPlan plan = plan_product(p.m, p.n, p.k, GATED != 0);
-    p.a_rows = plan.pair || p.m >= 128 ? 128 : (p.m + 7) / 8 * 8;
+    const uint32_t few = p.m >= 128 ? 128 : (p.m + 7) / 8 * 8;
+    const ProductPlan plan = plan_product<GATED>(p.m, p.n, p.k, few);
+    p.a_rows = plan.pair ? 128 : few;
     CUtensorMap map_a, map_b0, map_b1;
     if (const cudaError_t e = codes_map(&map_a, a, p.a_rows)) return e;
     if (const cudaError_t e = codes_map(&map_b0, b0, 128)) return e;
@@ -692,9 +804,10 @@ cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t
         return launch_clustered(mx_pair_kernel<GATED>, 2 * (tiles < pairs ? tiles : pairs), 0, kPairThreads, kPairSmem, stream, args);
     }
     p.tiles_m = (p.m + 127) / 128; p.tiles_n = (p.n + 127) / 128;
-    uint32_t split = plan.split;
-    void* args[] = {&map_a, &map_b0, &map_b1, &p, &split};
-    return launch_clustered(mx_split_kernel<GATED>, p.tiles_m * p.tiles_n * split, split, kSmallThreads, SmallShape<GATED>::kSmem, stream, args);
+    if (plan.split == 2) return launch_split_as<GATED, 2>(map_a, map_b0, map_b1, p, stream);
+    if (plan.split == 4) return launch_split_as<GATED, 4>(map_a, map_b0, map_b1, p, stream);
+    if constexpr (!GATED) if (plan.split == 8) return launch_split_as<0, 8>(map_a, map_b0, map_b1, p, stream);
+    return launch_split_as<GATED, 1>(map_a, map_b0, map_b1, p, stream);
 }
 
 }  // namespace
