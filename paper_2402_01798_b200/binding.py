@@ -440,10 +440,8 @@ def tq_mx_scale_stride(cols: int, layout: int = MX_TILES) -> int:
 
 def new_mx(rows: int, cols: int, layout: int = MX_TILES, device="cuda") -> MxMatrix:
     """Memory for a matrix, uninitialised; the calls that write one write all of it, the filling of its last scale tiles included."""
-    blocks = (cols + 31) // 32
-    tiles = layout == MX_TILES
-    codes = torch.empty((rows, blocks * 16), dtype=torch.uint8, device=device)
-    scales = torch.empty(((rows + 127) // 128, (blocks + 3) // 4 * 512) if tiles else (rows, (blocks + 15) // 16 * 16), dtype=torch.uint8, device=device)
+    index = device.index if isinstance(device, torch.device) else torch.device(device).index
+    codes, scales = _calls().new_mx(rows, cols, layout, torch.cuda.current_device() if index is None else index)
     return MxMatrix(codes, scales, rows, cols, layout)
 
 

@@ -144,16 +144,21 @@ __device__ __forceinline__ void stg256_words(void* p, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
                  :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "l"(p) : "memory");
 }
-// WIDTH consecutive elements of one row, 32, 16 or 8 of them; columns from n on are left out.
+// WIDTH consecutive elements of 32 rows, one row a thread: `row0` is the warp's first.  Where rows start on 16-byte boundaries and all columns exist
+// a thread stores its row; else eight columns at a time change places in `scratch` (the warp's 32 x 9 words), so that eight threads
+// store neighbours (32 scattered elements a store took 47 us for 300 x 300 x 8192).
+constexpr int kScratchWords = 32 * 9;
 template <int WIDTH>
-__device__ __forceinline__ void store_row(const ProductArgs& p, uint64_t row, uint64_t col, const float (&v)[WIDTH], uint32_t n, uint64_t offset) {
-    const bool whole = col + WIDTH <= n;
-    if (p.out_bf16) {
-        unsigned short* to = static_cast<unsigned short*>(p.out) + row * p.out_stride + offset + col;
-        uint32_t w[WIDTH / 2];
+__device__ __forceinline__ void store_rows(const ProductArgs& p, float* scratch, uint64_t row0, uint64_t col, const float (&v)[WIDTH], uint32_t n, uint64_t offset) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (p.out_wide >= 16 && col + WIDTH <= n) {
+        const uint64_t row = row0 + lane;
+        if (row >= p.m) return;
+        if (p.out_bf16) {
+            unsigned short* to = static_cast<unsigned short*>(p.out) + row * p.out_stride + offset + col;
+            uint32_t w[WIDTH / 2];
 #pragma unroll
-        for (int i = 0; i < WIDTH / 2; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        if (whole && p.out_wide >= 16) {
+            for (int i = 0; i < WIDTH / 2; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
             if (WIDTH >= 16 && p.out_wide == 32) {
 #pragma unroll
                 for (int i = 0; i < WIDTH / 16; ++i) {
@@ -165,13 +170,7 @@ __device__ __forceinline__ void store_row(const ProductArgs& p, uint64_t row, ui
                 for (int i = 0; i < WIDTH / 8; ++i) stg128(to + 8 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
             }
         } else {
-#pragma unroll
-            for (int i = 0; i < WIDTH; ++i)
-                if (col + i < n) to[i] = static_cast<unsigned short>(i & 1 ? w[i / 2] >> 16 : w[i / 2]);
-        }
-    } else {
-        float* to = static_cast<float*>(p.out) + row * p.out_stride + offset + col;
-        if (whole && p.out_wide >= 16) {
+            float* to = static_cast<float*>(p.out) + row * p.out_stride + offset + col;
             if (p.out_wide == 32) {
 #pragma unroll
                 for (int i = 0; i < WIDTH / 8; ++i) {
@@ -183,20 +182,38 @@ __device__ __forceinline__ void store_row(const ProductArgs& p, uint64_t row, ui
                 for (int i = 0; i < WIDTH / 4; ++i)
                     stg128(to + 4 * i, make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < WIDTH; ++i)
-                if (col + i < n) to[i] = v[i];
         }
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < WIDTH / 8; ++q) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) scratch[lane * 9 + e] = v[8 * q + e];
+        __syncwarp();
+        const uint64_t c = col + 8 * q + lane % 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t r = 4 * i + lane / 8;
+            const float x = scratch[r * 9 + lane % 8];
+            if (row0 + r < p.m && c < n) {
+                const uint64_t to = (row0 + r) * p.out_stride + offset + c;
+                if (p.out_bf16) static_cast<unsigned short*>(p.out)[to] = static_cast<unsigned short>(pack_bf16(x, 0.0f));
+                else static_cast<float*>(p.out)[to] = x;
+            }
+        }
+        __syncwarp();
     }
 }
-// One block of h from both projections: stores what is kept of them and the codes, returns the scale byte.
+// A block of h in each of 32 rows from both projections: stores what is kept of them and the codes, returns the scale byte (0 for a row that is not there).
 template <bool GELU>
-__device__ __forceinline__ uint32_t store_gated(const ProductArgs& p, uint64_t row, uint64_t f, const float (&g)[32], const float (&u)[32]) {
+__device__ __forceinline__ uint32_t store_gated(const ProductArgs& p, float* scratch, uint64_t row0, uint64_t f, const float (&g)[32], const float (&u)[32]) {
+    if (f >= p.n) return 0;
     if (p.out) {
-        store_row<32>(p, row, f, g, p.n, 0);
-        store_row<32>(p, row, f, u, p.n, p.n);
+        store_rows<32>(p, scratch, row0, f, g, p.n, 0);
+        store_rows<32>(p, scratch, row0, f, u, p.n, p.n);
     }
+    const uint64_t row = row0 + (threadIdx.x & 31);
+    if (row >= p.m) return 0;
     float h[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) h[i] = gate_value<GELU>(g[i]) * u[i];
@@ -236,6 +253,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
     __shared__ uint32_t tmem_base;
+    __shared__ float scratch[8][kScratchWords];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
     const uint32_t bars = base + kPairStages * kPairStage;
     const auto full = [&](int s) { return bars + 8 * s; };                           // first block: the loads of both
@@ -339,7 +357,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
             const uint32_t band = t % p.tiles_m * 2 + rank, n0 = t / p.tiles_m * kWide;
             if (!warp_wait(done, n_tile & 1, &dead)) break;
             fence_after();
-            const uint32_t local = quarter * 32 + lane, row = band * 128 + local;
+            const uint32_t local = quarter * 32 + lane, row0 = band * 128 + quarter * 32;
             const uint32_t from = tmem + (n_tile & 1) * kSecond + ((quarter * 32) << 16);
             const auto release = [&] {
                 fence_before();
@@ -356,7 +374,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
                     tmem_wait_loads();
                     if (i == 2 - half) release();
                     const uint32_t col = n0 + 32 * j;
-                    if (row < p.m && col < p.n) store_row<32>(p, row, col, v, p.n, 0);
+                    if (col < p.n) store_rows<32>(p, scratch[warp - 2], row0, col, v, p.n, 0);
                     __syncwarp();
                 }
             } else {
@@ -369,7 +387,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
                     tmem_load(from + 128 + 32 * j, u);
                     tmem_wait_loads();
                     if (i == 1) release();
-                    if (row < p.m && f < p.n) bytes |= store_gated<GATED == 2>(p, row, f, g, u) << (8 * i);
+                    bytes |= store_gated<GATED == 2>(p, scratch[warp - 2], row0, f, g, u) << (8 * i);
                     __syncwarp();
                 }
                 // every row of the 128, those behind the last token with zeros
@@ -438,6 +456,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     __shared__ volatile int dead;
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t barriers[2 * S::kMostStages + 2];
+    __shared__ float scratch[8][kScratchWords];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
     const uint32_t bars = smem_addr(barriers);
     const auto full = [&](uint32_t s) { return bars + 8 * s; };
@@ -529,7 +548,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
         __syncwarp();
     }
     // Two warps for each quarter of the lanes.
-    const uint32_t quarter = warp % 4, half = (warp - 2) / 4, local = quarter * 32 + lane, row = tm * 128 + local;
+    const uint32_t quarter = warp % 4, half = (warp - 2) / 4, local = quarter * 32 + lane, row0 = tm * 128 + quarter * 32;
     const uint32_t from = tmem + ((quarter * 32) << 16);
     const uint32_t rows = p.m - tm * 128 < 128 ? p.m - tm * 128 : 128;
     const bool taker = warp >= 2 && quarter * 32 < rows;        // has rows to take out of tensor memory
@@ -558,12 +577,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
                 tmem_load(from + 32 * j, v);
                 if constexpr (!GATED) {
                     tmem_wait_loads();
-                    if (row < p.m && col < p.n) store_row<32>(p, row, col, v, p.n, 0);
+                    if (col < p.n) store_rows<32>(p, scratch[warp - 2], row0, col, v, p.n, 0);
                 } else {
                     float u[32];
                     tmem_load(from + 128 + 32 * j, u);
                     tmem_wait_loads();
-                    if (row < p.m) put_scale(local, j, col < p.n ? store_gated<GATED == 2>(p, row, col, v, u) : 0);
+                    const uint32_t byte = store_gated<GATED == 2>(p, scratch[warp - 2], row0, col, v, u);
+                    if (local < rows) put_scale(local, j, byte);
                 }
                 __syncwarp();
             }
@@ -652,13 +672,14 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
             tmem_wait_loads();
             add_up(v, 0);
             if constexpr (!GATED) {
-                if (row < p.m && col < p.n) store_row<Q::kWidth>(p, row, col, v, p.n, 0);
+                if (col < p.n) store_rows<Q::kWidth>(p, scratch[warp - 2], row0, col, v, p.n, 0);
             } else {
                 float u[32];
                 tmem_load(from + 128 + rank * Q::kSlice + half * Q::kWidth, u);
                 tmem_wait_loads();
                 add_up(u, 8);
-                if (row < p.m) put_scale(local, rank * Q::kHalves + half, col < p.n ? store_gated<GATED == 2>(p, row, col, v, u) : 0);
+                const uint32_t byte = store_gated<GATED == 2>(p, scratch[warp - 2], row0, col, v, u);
+                if (local < rows) put_scale(local, rank * Q::kHalves + half, byte);
             }
         }
     }
@@ -733,7 +754,7 @@ ProductPlan plan_product(uint32_t m, uint32_t n, uint32_t k, uint32_t a_rows) {
     const uint64_t narrow = (static_cast<uint64_t>(m) + 127) / 128 * ((static_cast<uint64_t>(n) + 127) / 128);
     const uint32_t rows = m < 128 ? m : 128;
     for (uint32_t split = 1; split <= (GATED ? 4u : 8u) && split <= chunks; split *= 2) {
-        const bool two = !GATED && split_memory<GATED>(rows, a_rows, chunks, split).bytes <= 112 * 1024;
+        const bool two = !GATED && split_memory<GATED>(rows, a_rows, chunks, split).bytes <= 100 * 1024;      // beside 10 KB of fixed arrays
         const uint64_t room = (split == 8 ? sms * 7 / 8 : sms) * (two ? 2 : 1), blocks = narrow * split;
         const uint64_t waves = (blocks + room - 1) / room, stage = (GATED ? 340 : 285) + rows / 5 + 70 * (blocks < sms ? blocks : sms) / sms;
         const uint64_t sums = split == 1 ? 500 : 800 + 100 * split + 4 * rows * split;

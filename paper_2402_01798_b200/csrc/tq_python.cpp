@@ -4,6 +4,8 @@
 // 2.6 us of the launch, which bounds rounds of short gradients.
 #include <Python.h>
 
+#include <ATen/ops/as_strided.h>
+#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -442,6 +444,32 @@ Plain plain(const at::Tensor& t, const char* what, uint64_t rows, uint64_t cols)
     p.stride = have > 1 ? static_cast<uint64_t>(t.stride(0)) : wide;
     return p;
 }
+// Memory for a matrix: (codes, scales).  Rows of codes that are longer than 128 bytes start on such a boundary: the products load 128 bytes of a row at a time.
+PyObject* new_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {              // rows, cols, layout, device index
+    try {
+        Args a(args, n);
+        const uint64_t rows = a.u64(), cols = a.u64(), layout = a.u64();
+        const int64_t device = static_cast<int64_t>(a.u64());
+        if (rows >= (1ull << 31) || cols > (1ull << 40)) fail(PyExc_ValueError, "a matrix of this size is not possible");
+        const int64_t width = static_cast<int64_t>((cols + 31) / 32 * 16), high = static_cast<int64_t>(rows);
+        const int64_t stride = width > 128 ? (width + 127) / 128 * 128 : width;
+        const bool tiles = layout == TQ_MX_TILES;
+        const int64_t s_rows = tiles ? (high + 127) / 128 : high, s_width = tiles ? (width / 16 + 3) / 4 * 512 : (width / 16 + 15) / 16 * 16;
+        const auto options = at::TensorOptions().dtype(at::kByte).device(at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device)));
+        at::Tensor codes = at::empty({high, stride}, options), scales = at::empty({s_rows, s_width}, options);
+        if (stride != width) codes = codes.as_strided({high, width}, {stride, 1});
+        PyObject* pair = PyTuple_New(2);
+        if (!pair) return nullptr;
+        PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(std::move(codes)));
+        PyTuple_SET_ITEM(pair, 1, THPVariable_Wrap(std::move(scales)));
+        return pair;
+    } catch (const Failed&) {
+        return nullptr;
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
 tq_status mx_quantize(Args& a) {                // x, rounding, seed, first_row, out, stream
     const at::Tensor& x = a.tensor();
     const uint32_t rounding = a.u32();
@@ -531,6 +559,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define TQ_ENTRY(name) {#name, reinterpret_cast<PyCFunction>(entry<name>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(bind), METH_FASTCALL, nullptr},
+    {"new_mx", reinterpret_cast<PyCFunction>(new_mx), METH_FASTCALL, nullptr},
     TQ_ENTRY(stats), TQ_ENTRY(stats_hinted), TQ_ENTRY(stats_static), TQ_ENTRY(params_batch), TQ_ENTRY(params_device), TQ_ENTRY(compress),
     TQ_ENTRY(compress_device_params), TQ_ENTRY(decompress_aggregate), TQ_ENTRY(decompress_aggregate_rows), TQ_ENTRY(decompress_aggregate_apply),
     TQ_ENTRY(decompress_aggregate_device_params), TQ_ENTRY(stats_segments), TQ_ENTRY(stats_hinted_segments), TQ_ENTRY(compress_segments),
