@@ -51,7 +51,8 @@ __global__ void __launch_bounds__(kThreads) mx_rows_kernel(MxInput in, MxView ou
     float v[32];
     load_row_block<BF16>(in.data, row * in.stride + block * 32, true, out.cols - block * 32 < 32 ? static_cast<int>(out.cols - block * 32) : 32, v);
     const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
-    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&r)[4]) { mx_random8(first_row + static_cast<uint32_t>(row), block * 4 + q, keys, r); });
+    const PhiloxRun run = philox_run(static_cast<uint32_t>(block * 4 >> 32), first_row + static_cast<uint32_t>(row), keys);
+    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&r)[4]) { mx_random8(run, block * 4 + q, keys, r); });
     stg128(out.codes + row * out.code_stride + block * 16, codes);
     out.scales[mx_scale_at(out, row, block)] = static_cast<uint8_t>(byte);
 }
@@ -97,8 +98,9 @@ __device__ __forceinline__ void encode_row(MxTile& t, const MxItem& it, const fl
                                            const RoundKeys& keys, uint32_t first_row) {
     const uint64_t blocks = mx_blocks(out.cols), block = c0 / 32 + it.b;
     const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
+    const PhiloxRun run = philox_run(static_cast<uint32_t>(block * 4 >> 32), first_row + static_cast<uint32_t>(r0) + it.r, keys);
     const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&w)[4]) {
-        mx_random8(first_row + static_cast<uint32_t>(r0) + it.r, block * 4 + q, keys, w);
+        mx_random8(run, block * 4 + q, keys, w);
         if constexpr (KEEP) *reinterpret_cast<uint4*>(&t.random[random_chunk(it.r, it.b * 4 + q)]) = make_uint4(w[0], w[1], w[2], w[3]);
     });
     if (it.r < height && it.b * 32 < width) {
@@ -168,56 +170,65 @@ __global__ void __launch_bounds__(kThreads, 3) mx_tile_kernel(MxInput in, MxView
 }
 
 // ---- decoding ----------------------------------------------------------------------------------------------------
-// A thread makes 8 elements.  WIDE: it stores them in one piece; else the warp passes its codes around so that consecutive threads store
-// consecutive elements, for rows on any boundary.
+// A thread makes 8 elements in each of 4 rows.  WIDE: it stores them in one piece; else the warp passes its codes around so that consecutive threads
+// store consecutive elements, for rows on any boundary.  A block covers 8 << shift columns and 4 * (256 >> shift) rows.
+constexpr int kDecodeRows = 4;
 template <bool BF16, bool WIDE>
-__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxView m, void* out, uint64_t stride, uint32_t chunks) {
+__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxView m, void* out, uint64_t stride, uint32_t chunks, uint32_t shift) {
     pdl_wait();
-    const uint64_t row = blockIdx.x / chunks;
-    const uint64_t first = (static_cast<uint64_t>(blockIdx.x % chunks) * kThreads + (threadIdx.x & ~31u)) * 8;      // the warp's first element
-    if (first >= m.cols) return;
-    const uint64_t col = first + (threadIdx.x & 31) * 8;
+    const uint32_t high = kThreads >> shift;
+    const uint64_t row0 = static_cast<uint64_t>(blockIdx.x / chunks) * (high * kDecodeRows) + (threadIdx.x >> shift);
+    const uint64_t col = (static_cast<uint64_t>(blockIdx.x % chunks) << (shift + 3)) + (threadIdx.x & ((1u << shift) - 1)) * 8;
     const bool any = col < m.cols;
-    uint32_t codes = 0, byte = 0;
-    if (any) {
-        asm volatile("ld.global.b32 %0, [%1];" : "=r"(codes) : "l"(m.codes + row * m.code_stride + col / 2) : "memory");
-        byte = ldg8(m.scales + mx_scale_at(m, row, col / 32));
-    }
-    const float scale = mx_scale_value(byte);
-    char* const to = static_cast<char*>(out) + row * stride * (BF16 ? 2 : 4);
-    if constexpr (WIDE) {
-        if (!any) return;
-        float v[8];
-        e2m1_values8(codes, v);
+    uint32_t codes[kDecodeRows], byte[kDecodeRows];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= scale;
-        if (col + 8 <= m.cols) {
-            if constexpr (BF16) {
-                stg128(to + col * 2, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
-            } else {
-                stg128(to + col * 4, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
-                stg128(to + col * 4 + 16, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e < m.cols) {
-                    if constexpr (BF16) reinterpret_cast<unsigned short*>(to)[col + e] = static_cast<unsigned short>(__float_as_uint(v[e]) >> 16);   // exact
-                    else reinterpret_cast<float*>(to)[col + e] = v[e];
-                }
+    for (int i = 0; i < kDecodeRows; ++i) {
+        const uint64_t row = row0 + i * high;
+        codes[i] = byte[i] = 0;
+        if (any && row < m.rows) {
+            asm volatile("ld.global.b32 %0, [%1];" : "=r"(codes[i]) : "l"(m.codes + row * m.code_stride + col / 2) : "memory");
+            byte[i] = ldg8(m.scales + mx_scale_at(m, row, col / 32));
         }
-    } else {
-        const uint32_t lane = threadIdx.x & 31;
+    }
+    char* to = static_cast<char*>(out) + row0 * stride * (BF16 ? 2 : 4);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t w = __shfl_sync(0xFFFFFFFFu, codes, 4 * i + lane / 8);
-            const float s = __shfl_sync(0xFFFFFFFFu, scale, 4 * i + lane / 8);
+    for (int i = 0; i < kDecodeRows; ++i, to += high * stride * (BF16 ? 2 : 4)) {
+        if (row0 + i * high >= m.rows) continue;                 // a whole warp's, where warps exchange codes
+        const float scale = mx_scale_value(byte[i]);
+        if constexpr (WIDE) {
             float v[8];
-            e2m1_values8(w >> (4 * (lane & 7)), v);
-            const uint64_t c = first + 32 * i + lane;
-            if (c < m.cols) {
-                if constexpr (BF16) reinterpret_cast<unsigned short*>(to)[c] = static_cast<unsigned short>(__float_as_uint(v[0] * s) >> 16);
-                else reinterpret_cast<float*>(to)[c] = v[0] * s;
+            e2m1_values8(codes[i], v);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) unpair(mul2(pair(v[e], v[e + 1]), both(scale)), v[e], v[e + 1]);
+            if (col + 8 <= m.cols) {
+                if constexpr (BF16) {
+                    stg128(to + col * 2, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+                } else {
+                    stg128(to + col * 4, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+                    stg128(to + col * 4 + 16, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (col + e < m.cols) {
+                        if constexpr (BF16) reinterpret_cast<unsigned short*>(to)[col + e] = static_cast<unsigned short>(__float_as_uint(v[e]) >> 16);   // exact
+                        else reinterpret_cast<float*>(to)[col + e] = v[e];
+                    }
+            }
+        } else {                                                 // shift >= 5: a warp lies in one row
+            const uint32_t lane = threadIdx.x & 31;
+            const uint64_t first = col - lane * 8;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t w = __shfl_sync(0xFFFFFFFFu, codes[i], 4 * k + lane / 8);
+                const float s = __shfl_sync(0xFFFFFFFFu, scale, 4 * k + lane / 8);
+                float v[8];
+                e2m1_values8(w >> (4 * (lane & 7)), v);
+                const uint64_t c = first + 32 * k + lane;
+                if (c < m.cols) {
+                    if constexpr (BF16) reinterpret_cast<unsigned short*>(to)[c] = static_cast<unsigned short>(__float_as_uint(v[0] * s) >> 16);
+                    else reinterpret_cast<float*>(to)[c] = v[0] * s;
+                }
             }
         }
     }
@@ -227,37 +238,49 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxView m, void*
 struct MxWeights {
     float w[TQ_MAX_WORKERS];
 };
-// A thread decodes the same block of 32 elements of every worker's row and keeps the 32 sums.  fp32, in worker order.
-template <bool WEIGHTED>
+// A thread decodes the same EACH elements of every worker's row (32, a block; 8 where the rows are too short to fill the GPU so) and keeps their sums.
+// fp32, in worker order; code * scale is exact, so that one fused operation adds it.
+template <bool WEIGHTED, int EACH>
 __global__ void __launch_bounds__(kThreads) mx_aggregate_kernel(MxView m, float* out, uint32_t n, float divisor, MxWeights weights) {
     pdl_wait();
-    const uint64_t block = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (block * 32 >= m.cols) return;
-    float sum[32];
+    const uint64_t first = (static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x) * EACH;
+    if (first >= m.cols) return;
+    f32x2 sum[EACH / 2];
 #pragma unroll
-    for (int e = 0; e < 32; ++e) sum[e] = 0.0f;
+    for (int e = 0; e < EACH / 2; ++e) sum[e] = both(0.0f);
+    const uint8_t* codes = m.codes + first / 2;
+    const uint8_t* scales = m.scales + first / 32;
 #pragma unroll 4
-    for (uint32_t i = 0; i < n; ++i) {
-        const uint4 c = ldg128(m.codes + i * m.code_stride + block * 16);
-        const float scale = mx_scale_value(ldg8(m.scales + i * m.scale_stride + block));
-        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    for (uint32_t i = 0; i < n; ++i, codes += m.code_stride, scales += m.scale_stride) {
+        uint32_t w[EACH / 8];
+        if constexpr (EACH == 32) {
+            const uint4 c = ldg128(codes);
+            w[0] = c.x; w[1] = c.y; w[2] = c.z; w[3] = c.w;
+        } else {
+            asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(codes) : "memory");
+        }
+        const f32x2 scale = both(mx_scale_value(ldg8(scales)));
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < EACH / 8; ++q) {
             float v[8];
             e2m1_values8(w[q], v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = v[e] * scale;
-                sum[8 * q + e] += WEIGHTED ? x * weights.w[i] : x;
+            for (int e = 0; e < 4; ++e) {
+                f32x2& to = sum[4 * q + e];
+                if constexpr (WEIGHTED) to = add2(to, mul2(mul2(pair(v[2 * e], v[2 * e + 1]), scale), both(weights.w[i])));
+                else to = fma2(pair(v[2 * e], v[2 * e + 1]), scale, to);
             }
         }
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < EACH / 8; ++q) {
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = WEIGHTED ? sum[8 * q + e] : __fdiv_rn(sum[8 * q + e], divisor);
-        const uint64_t col = block * 32 + 8 * q;
+        for (int e = 0; e < 4; ++e) {
+            unpair(sum[4 * q + e], v[2 * e], v[2 * e + 1]);
+            if constexpr (!WEIGHTED) { v[2 * e] = __fdiv_rn(v[2 * e], divisor); v[2 * e + 1] = __fdiv_rn(v[2 * e + 1], divisor); }
+        }
+        const uint64_t col = first + 8 * q;
         if (col + 8 <= m.cols) stg256(out + col, v);
         else
 #pragma unroll
@@ -375,12 +398,14 @@ cudaError_t launch_mx_quantize(const MxQuantizeCall& c) {
 }
 
 cudaError_t launch_mx_dequantize(const tq_mx_t& m, void* out, bool bf16, uint64_t stride, cudaStream_t stream) {
-    const uint64_t chunks = (m.cols + kThreads * 8 - 1) / (kThreads * 8);
-    const dim3 grid(static_cast<unsigned>(chunks * m.rows));
     const bool wide = (reinterpret_cast<uintptr_t>(out) | (m.rows > 1 ? stride * (bf16 ? 2 : 4) : 0)) % 16 == 0;
+    uint32_t shift = wide ? 2 : 5;
+    while (shift < 8 && (8ull << shift) < m.cols) ++shift;
+    const uint64_t chunks = (m.cols + (8ull << shift) - 1) >> (shift + 3), high = static_cast<uint64_t>(kThreads >> shift) * kDecodeRows;
+    const dim3 grid(static_cast<unsigned>(chunks * ((m.rows + high - 1) / high)));
     auto* kernel = bf16 ? (wide ? mx_dequantize_kernel<true, true> : mx_dequantize_kernel<true, false>)
                         : (wide ? mx_dequantize_kernel<false, true> : mx_dequantize_kernel<false, false>);
-    return launch_kernel(kernel, grid, kThreads, 0, stream, mx_view(m), out, stride, static_cast<uint32_t>(chunks));
+    return launch_kernel(kernel, grid, kThreads, 0, stream, mx_view(m), out, stride, static_cast<uint32_t>(chunks), shift);
 }
 
 cudaError_t launch_mx_aggregate(const tq_mx_t& m, const float* weights, float* out, cudaStream_t stream) {
@@ -388,8 +413,11 @@ cudaError_t launch_mx_aggregate(const tq_mx_t& m, const float* weights, float* o
     const uint32_t n = static_cast<uint32_t>(m.rows);
     if (weights)
         for (uint32_t i = 0; i < n; ++i) w.w[i] = weights[i];
-    const dim3 grid(static_cast<unsigned>((mx_blocks(m.cols) + kThreads - 1) / kThreads));
-    auto* kernel = weights ? mx_aggregate_kernel<true> : mx_aggregate_kernel<false>;
+    const bool shortened = mx_blocks(m.cols) < static_cast<uint64_t>(sm_count()) * kThreads * 2;
+    const uint64_t each = shortened ? 8 : 32;
+    const dim3 grid(static_cast<unsigned>((m.cols + each * kThreads - 1) / (each * kThreads)));
+    auto* kernel = shortened ? (weights ? mx_aggregate_kernel<true, 8> : mx_aggregate_kernel<false, 8>)
+                             : (weights ? mx_aggregate_kernel<true, 32> : mx_aggregate_kernel<false, 32>);
     return launch_kernel(kernel, grid, kThreads, 0, stream, mx_view(m), out, n, static_cast<float>(n), w);
 }
 
