@@ -445,6 +445,12 @@ def new_mx(rows: int, cols: int, layout: int = MX_TILES, device="cuda") -> MxMat
     return MxMatrix(codes, scales, rows, cols, layout)
 
 
+def _new_plain(like: torch.Tensor, rows: Optional[int], cols: int, dtype: torch.dtype) -> torch.Tensor:
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise TypeError("float32 or bfloat16 is needed")
+    return _calls().new_plain(like, rows, cols, dtype is torch.bfloat16)
+
+
 def _seed(seed: int) -> int:
     return seed & 0xFFFFFFFFFFFFFFFF
 
@@ -472,7 +478,7 @@ def tq_mx_quantize_both(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int =
 def tq_mx_dequantize(m: MxMatrix, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The values of ``m`` as a [rows, cols] tensor."""
     if out is None:
-        out = torch.empty((m.rows, m.cols), dtype=dtype, device=m.codes.device)
+        out = _new_plain(m.codes, m.rows, m.cols, dtype)
     _check(_calls().mx_dequantize(m, out, stream), "tq_mx_dequantize")
     return out
 
@@ -480,7 +486,7 @@ def tq_mx_dequantize(m: MxMatrix, dtype: torch.dtype = torch.float32, out: Optio
 def tq_mx_decompress_aggregate(m: MxMatrix, weights: Optional[Sequence[float]] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue the mean (or weighted sum) of the rows of ``m`` (layout MX_ROWS); returns the [cols] fp32 update."""
     if out is None:
-        out = torch.empty(m.cols, dtype=torch.float32, device=m.codes.device)
+        out = _new_plain(m.codes, None, m.cols, torch.float32)
     _check(_calls().mx_decompress_aggregate(m, weights, out, stream), "tq_mx_decompress_aggregate")
     return out
 
@@ -488,7 +494,7 @@ def tq_mx_decompress_aggregate(m: MxMatrix, weights: Optional[Sequence[float]] =
 def tq_mx_product(a: MxMatrix, b: MxMatrix, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue a b^T; returns [a.rows, b.rows]."""
     if out is None:
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.codes.device)
+        out = _new_plain(a.codes, a.rows, b.rows, dtype)
     _check(_calls().mx_product(a, b, out, stream), "tq_mx_product")
     return out
 

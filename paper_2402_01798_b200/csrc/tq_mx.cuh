@@ -71,14 +71,25 @@ __device__ __forceinline__ uint32_t e2m1_nearest8(const float (&v)[8]) {
 // products are exact, each is rounded once to an integer, 2^17 and 2^18 are even, and rounding keeps the order).  The code is
 // (P + 65535 - r) >> 16, one up when r < rint(p 2^16): byte 2 of the sum.  (By the exponent of a: four operations of the integer pipe, here one; rows of
 // 8192 x 4096 bf16 30 -> 21 us.)
-// `inverted` holds ~r for two elements in a word.
 __device__ __forceinline__ float min3(float a, float b, float c) { float r; asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // Byte 3 of four words.
 __device__ __forceinline__ uint32_t byte3_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0073u), __byte_perm(c, d, 0x0073u), 0x5410u);
 }
+// Where the inverted bits of an element are: in which word, and in which half of it (0x0001 the lower, 0x0100 the upper one).
+struct RowBits {                   // of 8 neighbours, two in a word
+    uint32_t w[4];
+    __device__ __forceinline__ uint32_t word(int e) const { return w[e >> 1]; }
+    __device__ __forceinline__ uint32_t half(int e) const { return e & 1 ? 0x0100u : 0x0001u; }
+};
+struct ColumnBits {                // of 8 elements in a column, each beside that of the next or last column
+    uint32_t w[8], side;
+    __device__ __forceinline__ uint32_t word(int e) const { return w[e]; }
+    __device__ __forceinline__ uint32_t half(int) const { return side; }
+};
 // Eight elements x, to be scaled by `inv`.
-__device__ __forceinline__ uint32_t e2m1_stochastic8(const float* x, float inv, const uint32_t (&inverted)[4]) {
+template <class Bits>
+__device__ __forceinline__ uint32_t e2m1_stochastic8(const float* x, float inv, const Bits& bits) {
     uint32_t s[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -87,8 +98,8 @@ __device__ __forceinline__ uint32_t e2m1_stochastic8(const float* x, float inv, 
         unpair(fma2(a, both(131072.0f), both(kMagic)), l[0], h[0]);
         unpair(fma2(a, both(65536.0f), both(kMagic + 131072.0f)), l[1], h[1]);
         unpair(fma2(a, both(32768.0f), both(kMagic + 262144.0f)), l[2], h[2]);
-        s[2 * i] = dot_halves(inverted[i], 0x0001u, __float_as_uint(min3(l[0], l[1], l[2])));
-        s[2 * i + 1] = dot_halves(inverted[i], 0x0100u, __float_as_uint(min3(h[0], h[1], h[2])));
+        s[2 * i] = dot_halves(bits.word(2 * i), bits.half(2 * i), __float_as_uint(min3(l[0], l[1], l[2])));
+        s[2 * i + 1] = dot_halves(bits.word(2 * i + 1), bits.half(2 * i + 1), __float_as_uint(min3(h[0], h[1], h[2])));
     }
     const uint32_t even = byte3_of(__float_as_uint(x[0]), __float_as_uint(x[2]), __float_as_uint(x[4]), __float_as_uint(x[6]));
     const uint32_t odd = byte3_of(__float_as_uint(x[1]), __float_as_uint(x[3]), __float_as_uint(x[5]), __float_as_uint(x[7]));
@@ -108,13 +119,14 @@ __device__ __forceinline__ void e2m1_values8(uint32_t codes, float (&v)[8]) {
 
 // Random bits of the elements (row, 8 * group .. 8 * group + 7), inverted: word i holds those of elements 2i (low half) and 2i + 1.
 // `run` belongs to the row and the group's upper half.
-__device__ __forceinline__ void mx_random8(const PhiloxRun& run, uint64_t group, const RoundKeys& keys, uint32_t (&out)[4]) {
-    philox_block(static_cast<uint32_t>(group), run, keys, out);
+__device__ __forceinline__ void mx_random8(const PhiloxRun& run, uint64_t group, const RoundKeys& keys, RowBits& out) {
+    philox_block(static_cast<uint32_t>(group), run, keys, out.w);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = ~out[i];
+    for (int i = 0; i < 4; ++i) out.w[i] = ~out.w[i];
 }
 
-// 32 elements -> their 32 codes, element 0 in the lowest nibble.  `random(q, out)` gives the inverted bits of elements 8q .. 8q + 7.
+// 32 elements -> their 32 codes, element 0 in the lowest nibble.  `random(q)` gives the bits of elements 8q .. 8q + 7 (RowBits or
+// ColumnBits); it is not called for nearest rounding.
 template <bool STOCHASTIC, class Random>
 __device__ __forceinline__ uint4 mx_encode32(const float (&v)[32], uint32_t byte, Random random) {
     uint32_t w[4];
@@ -122,9 +134,7 @@ __device__ __forceinline__ uint4 mx_encode32(const float (&v)[32], uint32_t byte
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if constexpr (STOCHASTIC) {
-            uint32_t r[4];
-            random(q, r);
-            w[q] = e2m1_stochastic8(&v[8 * q], inv, r);
+            w[q] = e2m1_stochastic8(&v[8 * q], inv, random(q));
         } else {
             float y[8];
 #pragma unroll
@@ -144,6 +154,10 @@ __device__ __forceinline__ void stg128(void* p, uint4 v) {
 }
 __device__ __forceinline__ uint4 ldg128(const void* p) {
     uint4 v; asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory"); return v;
+}
+__device__ __forceinline__ void ldg256(const void* p, uint32_t (&v)[8]) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p) : "memory");
 }
 __device__ __forceinline__ uint32_t ldg8(const void* p) {
     uint32_t v; asm volatile("ld.global.b8 %0, [%1];" : "=r"(v) : "l"(p) : "memory"); return v;

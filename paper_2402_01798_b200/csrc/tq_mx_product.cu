@@ -218,7 +218,7 @@ __device__ __forceinline__ uint32_t store_gated(const ProductArgs& p, float* scr
 #pragma unroll
     for (int i = 0; i < 32; ++i) h[i] = gate_value<GELU>(g[i]) * u[i];
     const uint32_t byte = mx_scale_byte<false>(max_abs_32(h));
-    stg128(p.h.codes + row * p.h.code_stride + f / 2, mx_encode32<false>(h, byte, [](int, uint32_t (&)[4]) {}));
+    stg128(p.h.codes + row * p.h.code_stride + f / 2, mx_encode32<false>(h, byte, [](int) { return RowBits{}; }));
     return byte;
 }
 

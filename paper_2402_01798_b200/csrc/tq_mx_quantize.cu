@@ -1,5 +1,7 @@
 // Microscaled 4-bit floating point: quantisation along one or both axes, decoding, the mean of decoded rows, and the backward
 // pass of the gated block's activation, which ends in three quantised matrices.
+#include <cstddef>
+
 #include "tq_mx.cuh"
 
 namespace tq {
@@ -9,14 +11,25 @@ namespace {
 struct MxInput {
     const void* data;
     uint64_t stride;               // elements from row to row
-    uint32_t wide;                 // 1: every row starts on a 16-byte boundary
+    uint32_t wide;                 // the boundary that every row starts on: 32 bytes, 16, or 0 for any
 };
 
-// A row block of 32 elements of the matrix from memory, zeros outside.  `wide`: the row starts on a 16-byte boundary.
+// A row block of 32 elements of the matrix from memory, zeros outside.  `wide`: the boundary that rows start on, 32 bytes, 16 or 0 for any.
 template <bool BF16>
-__device__ __forceinline__ void load_row_block(const void* data, uint64_t at, bool wide, int count, float (&v)[32]) {
+__device__ __forceinline__ void load_row_block(const void* data, uint64_t at, uint32_t wide, int count, float (&v)[32]) {
     const char* src = static_cast<const char*>(data) + at * (BF16 ? 2 : 4);
-    if (wide && count >= 32) {
+    if (wide == 32 && count >= 32) {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 2 : 4); ++i) {
+            uint32_t x[8];
+            ldg256(src + 32 * i, x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if constexpr (BF16) { v[16 * i + 2 * k] = __uint_as_float(x[k] << 16); v[16 * i + 2 * k + 1] = __uint_as_float(x[k] & 0xFFFF0000u); }
+                else v[8 * i + k] = __uint_as_float(x[k]);
+            }
+        }
+    } else if (wide && count >= 32) {
 #pragma unroll
         for (int i = 0; i < (BF16 ? 4 : 8); ++i) {
             const uint4 w = ldg128(src + 16 * i);
@@ -36,9 +49,10 @@ __device__ __forceinline__ void load_row_block(const void* data, uint64_t at, bo
 
 // ---- along the rows ----------------------------------------------------------------------------------------
 // One thread makes one block: 64 or 128 bytes in, 16 bytes of codes and a byte of scale out, no exchange between threads.
-// A block of 256 threads covers 2^shift MX blocks of 256 >> shift rows.  Bound by memory where rounding is to nearest.
+// A block of 256 threads covers 2^shift MX blocks of 256 >> shift rows.  16 x 25.6 M fp32, stochastic: 304 us, 6.1 TB/s, with four blocks an SM (64
+// registers); 383 us with three.
 template <bool BF16, bool STOCHASTIC>
-__global__ void __launch_bounds__(kThreads) mx_rows_kernel(MxInput in, MxView out, uint32_t shift, uint64_t col_groups, RoundKeys keys, uint32_t first_row) {
+__global__ void __launch_bounds__(kThreads, 4) mx_rows_kernel(MxInput in, MxView out, uint32_t shift, uint64_t col_groups, RoundKeys keys, uint32_t first_row) {
     pdl_wait();
     const uint64_t row = (blockIdx.x / col_groups) * (kThreads >> shift) + (threadIdx.x >> shift);
     const uint64_t block = (blockIdx.x % col_groups << shift) + (threadIdx.x & ((1u << shift) - 1));
@@ -49,10 +63,14 @@ __global__ void __launch_bounds__(kThreads) mx_rows_kernel(MxInput in, MxView ou
         return;
     }
     float v[32];
-    load_row_block<BF16>(in.data, row * in.stride + block * 32, true, out.cols - block * 32 < 32 ? static_cast<int>(out.cols - block * 32) : 32, v);
+    load_row_block<BF16>(in.data, row * in.stride + block * 32, in.wide, out.cols - block * 32 < 32 ? static_cast<int>(out.cols - block * 32) : 32, v);
     const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
     const PhiloxRun run = philox_run(static_cast<uint32_t>(block * 4 >> 32), first_row + static_cast<uint32_t>(row), keys);
-    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&r)[4]) { mx_random8(run, block * 4 + q, keys, r); });
+    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q) {
+        RowBits r;
+        mx_random8(run, block * 4 + q, keys, r);
+        return r;
+    });
     stg128(out.codes + row * out.code_stride + block * 16, codes);
     out.scales[mx_scale_at(out, row, block)] = static_cast<uint8_t>(byte);
 }
@@ -60,18 +78,20 @@ __global__ void __launch_bounds__(kThreads) mx_rows_kernel(MxInput in, MxView ou
 // ---- tiles in shared memory ------------------------------------------------------------------------------------
 // 64 x 128 elements, one block of 32 along a row and one along a column for each of 256 threads.  The thread makes its row block from
 // registers and leaves the elements in shared memory in fp32 for the thread that makes the column block.  32 elements are followed by
-// 4 words of padding: the 16-byte accesses of eight threads (two rows, four blocks) then touch different banks, as do those of 32
-// threads down 32 columns.  53 KB with the random bits: four blocks an SM, so that loads of one run beside the arithmetic of others.
+// 4 words of padding, 32 rows by 16: the 16-byte accesses of eight threads (two rows, four blocks) then touch different banks, as do those of 32
+// threads down 16 columns in both halves of the rows.  Two threads so hold the neighbouring 16 bytes of a transposed row, and stores fill sectors.
+// 53 KB with the random bits: four blocks an SM, so that loads of one run beside the arithmetic of others.
 constexpr int kTileRows = 64, kTileCols = 128;
 constexpr int kTilePitch = 4 * 36;
 struct MxTile {
-    float v[kTileRows * kTilePitch];
-    uint32_t random[kTileRows * 64];       // 16 bits an element, in 16-byte chunks of 8; see random_chunk
+    float v[kTileRows * kTilePitch + 16];
+    uint32_t random[kTileRows * 64 + 8];   // 16 bits an element, inverted, in 16-byte chunks of 8; see random_chunk.  Not there where rounding is to nearest
 };
-__device__ __forceinline__ int tile_at(int r, int c) { return r * kTilePitch + (c >> 5) * 36 + (c & 31); }
+constexpr size_t tile_bytes(bool stochastic) { return stochastic ? sizeof(MxTile) : offsetof(MxTile, random); }
+__device__ __forceinline__ int tile_at(int r, int c) { return r * kTilePitch + (r >> 5) * 16 + (c >> 5) * 36 + (c & 31); }
 // Word of the 16-byte chunk with the bits of row r, columns 8g .. 8g + 7.  The exchange of chunks keeps eight threads that write (two rows,
 // four blocks) in different banks.
-__device__ __forceinline__ int random_chunk(int r, int g) { return r * 64 + ((g ^ ((g >> 3) | ((r & 1) << 1))) << 2); }
+__device__ __forceinline__ int random_chunk(int r, int g) { return r * 64 + (r >> 5) * 8 + ((g ^ ((g >> 3) | ((r & 1) << 1))) << 2); }
 
 // This thread's row block: row r, block b of the tile.
 struct MxItem {
@@ -99,9 +119,11 @@ __device__ __forceinline__ void encode_row(MxTile& t, const MxItem& it, const fl
     const uint64_t blocks = mx_blocks(out.cols), block = c0 / 32 + it.b;
     const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
     const PhiloxRun run = philox_run(static_cast<uint32_t>(block * 4 >> 32), first_row + static_cast<uint32_t>(r0) + it.r, keys);
-    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&w)[4]) {
-        mx_random8(run, block * 4 + q, keys, w);
-        if constexpr (KEEP) *reinterpret_cast<uint4*>(&t.random[random_chunk(it.r, it.b * 4 + q)]) = make_uint4(w[0], w[1], w[2], w[3]);
+    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q) {
+        RowBits r;
+        mx_random8(run, block * 4 + q, keys, r);
+        if constexpr (KEEP) *reinterpret_cast<uint4*>(&t.random[random_chunk(it.r, it.b * 4 + q)]) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+        return r;
     });
     if (it.r < height && it.b * 32 < width) {
         stg128(out.codes + (r0 + it.r) * out.code_stride + block * 16, codes);
@@ -115,20 +137,18 @@ __device__ __forceinline__ void encode_row(MxTile& t, const MxItem& it, const fl
 // `fill`: the tile ends `out` below, and the rest of its last 128 rows gets zero scales.
 template <bool STOCHASTIC>
 __device__ __forceinline__ void encode_col(const MxTile& t, const MxView& out, uint64_t q0, uint64_t r0, int height, int width, bool fill) {
-    const int c = threadIdx.x & (kTileCols - 1), b = threadIdx.x >> 7;
+    const int c = threadIdx.x >> 1, b = threadIdx.x & 1;
     const uint64_t blocks = mx_blocks(out.cols), block = r0 / 32 + b, row = q0 + c;
     float v[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = t.v[tile_at(b * 32 + i, c)];
     const uint32_t byte = mx_scale_byte<STOCHASTIC>(max_abs_32(v));
-    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q, uint32_t (&w)[4]) {
-        const unsigned short* random = reinterpret_cast<const unsigned short*>(t.random);
+    const uint4 codes = mx_encode32<STOCHASTIC>(v, byte, [&](int q) {
+        ColumnBits r;
+        r.side = c & 1 ? 0x0100u : 0x0001u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = b * 32 + q * 8 + 2 * i;
-            const uint32_t lo = random[2 * random_chunk(r, c >> 3) + (c & 7)], hi = random[2 * random_chunk(r + 1, c >> 3) + (c & 7)];
-            w[i] = lo | (hi << 16);
-        }
+        for (int i = 0; i < 8; ++i) r.w[i] = t.random[random_chunk(b * 32 + q * 8 + i, c >> 3) + ((c & 7) >> 1)];
+        return r;
     });
     if (c < width && b * 32 < height) {
         stg128(out.codes + row * out.code_stride + block * 16, codes);
@@ -143,7 +163,7 @@ __device__ __forceinline__ int within(uint64_t size, uint64_t from, int most) {
 }
 
 template <bool BF16, bool STOCHASTIC, bool BOTH>
-__global__ void __launch_bounds__(kThreads, 3) mx_tile_kernel(MxInput in, MxView out, MxView out_t, uint32_t tiles_across, RoundKeys keys, uint32_t first_row) {
+__global__ void __launch_bounds__(kThreads, 4) mx_tile_kernel(MxInput in, MxView out, MxView out_t, uint32_t tiles_across, RoundKeys keys, uint32_t first_row) {
     extern __shared__ __align__(16) unsigned char raw[];
     MxTile& t = *reinterpret_cast<MxTile*>(raw);
     pdl_wait();
@@ -152,13 +172,23 @@ __global__ void __launch_bounds__(kThreads, 3) mx_tile_kernel(MxInput in, MxView
     const MxItem it = row_item();
     float v[32];
     if (in.wide) {
-        load_row_block<BF16>(in.data, (r0 + it.r) * in.stride + c0 + it.b * 32, true, it.r < height ? width - it.b * 32 : 0, v);
+        load_row_block<BF16>(in.data, (r0 + it.r) * in.stride + c0 + it.b * 32, in.wide, it.r < height ? width - it.b * 32 : 0, v);
         if constexpr (BOTH) put_row(t, it, v);
     } else {                               // rows on any boundary: one element a thread at a time, neighbours side by side
-        const int c = threadIdx.x % kTileCols;
-#pragma unroll 16
-        for (int r = threadIdx.x / kTileCols; r < kTileRows; r += kThreads / kTileCols)
-            t.v[tile_at(r, c)] = r < height && c < width ? load1<BF16>(in.data, (r0 + r) * in.stride + c0 + c) : 0.0f;
+        const int c = threadIdx.x % kTileCols, first = threadIdx.x / kTileCols;
+        const char* src = static_cast<const char*>(in.data) + ((r0 + first) * in.stride + c0 + c) * (BF16 ? 2 : 4);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {             // 16 loads, then 16 stores: in turn they took 91 us for 8191 x 5003 fp32 along both axes, so 67
+            float x[kTileRows / 4];
+#pragma unroll
+            for (int i = 0; i < kTileRows / 4; ++i) {
+                x[i] = 0.0f;
+                if (first + (half * kTileRows / 4 + i) * 2 < height && c < width) x[i] = load1<BF16>(src, 0);
+                src += in.stride * (BF16 ? 4 : 8);
+            }
+#pragma unroll
+            for (int i = 0; i < kTileRows / 4; ++i) t.v[tile_at(first + (half * kTileRows / 4 + i) * 2, c)] = x[i];
+        }
         __syncthreads();
         get_row(t, it, v);
     }
@@ -296,7 +326,7 @@ struct MxGatedInput {
     const void* dh;
     const void* gu;                // [tokens][>= 2 features]: g, then u
     uint64_t dh_stride, gu_stride, features;
-    uint32_t wide;                 // 1: all rows start on 16-byte boundaries
+    uint32_t wide;                 // the boundary that all rows start on: 32 bytes, 16, or 0 for any
 };
 template <bool BF16, bool GELU, bool STOCHASTIC>
 __global__ void __launch_bounds__(kThreads, 2) mx_gated_backward_kernel(MxGatedInput in, MxView dgu, MxView dgu_t, MxView h_t, uint32_t tiles_across, RoundKeys keys) {
@@ -350,10 +380,12 @@ cudaError_t allow_smem(K* kernel, size_t bytes) {
     return cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
 }
 
+uint32_t boundary(uint64_t at) { return at % 32 == 0 ? 32 : at % 16 == 0 ? 16 : 0; }
+
 template <bool BF16, bool STOCHASTIC>
 cudaError_t launch_quantize_as(const MxQuantizeCall& c) {
     const uint64_t rows = c.out->rows, cols = c.out->cols;
-    const MxInput in{c.x, c.x_stride, (reinterpret_cast<uintptr_t>(c.x) | (rows > 1 ? c.x_stride * (BF16 ? 2 : 4) : 0)) % 16 == 0};
+    const MxInput in{c.x, c.x_stride, boundary(reinterpret_cast<uintptr_t>(c.x) | (rows > 1 ? c.x_stride * (BF16 ? 2 : 4) : 0))};
     const MxView out = mx_view(*c.out), out_t = c.out_t ? mx_view(*c.out_t) : MxView{};
     const RoundKeys keys = round_keys(c.seed);
     if (!c.out_t && in.wide) {
@@ -367,11 +399,11 @@ cudaError_t launch_quantize_as(const MxQuantizeCall& c) {
     const uint64_t across = (cols + kTileCols - 1) / kTileCols, down = (rows + 127) / 128 * 2;       // whole scale tiles
     const dim3 grid(static_cast<unsigned>(across * down));
     if (c.out_t) {
-        if (const cudaError_t e = allow_smem(mx_tile_kernel<BF16, STOCHASTIC, true>, sizeof(MxTile))) return e;
-        return launch_kernel(mx_tile_kernel<BF16, STOCHASTIC, true>, grid, kThreads, sizeof(MxTile), c.stream, in, out, out_t, static_cast<uint32_t>(across), keys, c.first_row);
+        if (const cudaError_t e = allow_smem(mx_tile_kernel<BF16, STOCHASTIC, true>, tile_bytes(STOCHASTIC))) return e;
+        return launch_kernel(mx_tile_kernel<BF16, STOCHASTIC, true>, grid, kThreads, tile_bytes(STOCHASTIC), c.stream, in, out, out_t, static_cast<uint32_t>(across), keys, c.first_row);
     }
-    if (const cudaError_t e = allow_smem(mx_tile_kernel<BF16, STOCHASTIC, false>, sizeof(MxTile))) return e;
-    return launch_kernel(mx_tile_kernel<BF16, STOCHASTIC, false>, grid, kThreads, sizeof(MxTile), c.stream, in, out, out_t, static_cast<uint32_t>(across), keys, c.first_row);
+    if (const cudaError_t e = allow_smem(mx_tile_kernel<BF16, STOCHASTIC, false>, tile_bytes(STOCHASTIC))) return e;
+    return launch_kernel(mx_tile_kernel<BF16, STOCHASTIC, false>, grid, kThreads, tile_bytes(STOCHASTIC), c.stream, in, out, out_t, static_cast<uint32_t>(across), keys, c.first_row);
 }
 
 template <bool BF16, bool GELU, bool STOCHASTIC>
@@ -379,10 +411,10 @@ cudaError_t launch_gated_backward_as(const MxGatedBackwardCall& c) {
     const uint64_t features = c.h_t->rows, across = (features + kTileCols - 1) / kTileCols, down = (c.dgu->rows + 127) / 128 * 2;
     const uint64_t size = BF16 ? 2 : 4;
     const MxGatedInput in{c.dh, c.gu, c.dh_stride, c.gu_stride, features,
-                          (reinterpret_cast<uintptr_t>(c.dh) | reinterpret_cast<uintptr_t>(c.gu) | (c.dgu->rows > 1 ? (c.dh_stride | c.gu_stride) * size : 0)) % 16 == 0};
+                          boundary(reinterpret_cast<uintptr_t>(c.dh) | reinterpret_cast<uintptr_t>(c.gu) | (c.dgu->rows > 1 ? (c.dh_stride | c.gu_stride) * size : 0))};
     auto* kernel = mx_gated_backward_kernel<BF16, GELU, STOCHASTIC>;
-    if (const cudaError_t e = allow_smem(kernel, sizeof(MxTile))) return e;
-    return launch_kernel(kernel, dim3(static_cast<unsigned>(across * down)), kThreads, sizeof(MxTile), c.stream, in, mx_view(*c.dgu), mx_view(*c.dgu_t), mx_view(*c.h_t),
+    if (const cudaError_t e = allow_smem(kernel, tile_bytes(STOCHASTIC))) return e;
+    return launch_kernel(kernel, dim3(static_cast<unsigned>(across * down)), kThreads, tile_bytes(STOCHASTIC), c.stream, in, mx_view(*c.dgu), mx_view(*c.dgu_t), mx_view(*c.h_t),
                          static_cast<uint32_t>(across), round_keys(c.seed));
 }
 template <bool BF16, bool GELU>

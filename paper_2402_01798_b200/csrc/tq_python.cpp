@@ -444,6 +444,27 @@ Plain plain(const at::Tensor& t, const char* what, uint64_t rows, uint64_t cols)
     p.stride = have > 1 ? static_cast<uint64_t>(t.stride(0)) : wide;
     return p;
 }
+// A plain matrix on the device of a tensor; rows None: a vector.
+PyObject* new_plain(PyObject*, PyObject* const* args, Py_ssize_t n) {           // like, rows, cols, bf16
+    try {
+        Args a(args, n);
+        const at::Tensor& like = a.tensor();
+        PyObject* r = a.next();
+        int64_t rows = 0;
+        if (r != Py_None) {
+            rows = PyLong_AsLongLong(r);
+            if (rows == -1 && PyErr_Occurred()) throw Failed();
+        }
+        const int64_t cols = static_cast<int64_t>(a.u64());
+        const auto options = at::TensorOptions().dtype(a.u32() ? at::kBFloat16 : at::kFloat).device(like.device());
+        return THPVariable_Wrap(r == Py_None ? at::empty({cols}, options) : at::empty({rows, cols}, options));
+    } catch (const Failed&) {
+        return nullptr;
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
 // Memory for a matrix: (codes, scales).  Rows of codes that are longer than 128 bytes start on such a boundary: the products load 128 bytes of a row at a time.
 PyObject* new_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {              // rows, cols, layout, device index
     try {
@@ -560,6 +581,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(bind), METH_FASTCALL, nullptr},
     {"new_mx", reinterpret_cast<PyCFunction>(new_mx), METH_FASTCALL, nullptr},
+    {"new_plain", reinterpret_cast<PyCFunction>(new_plain), METH_FASTCALL, nullptr},
     TQ_ENTRY(stats), TQ_ENTRY(stats_hinted), TQ_ENTRY(stats_static), TQ_ENTRY(params_batch), TQ_ENTRY(params_device), TQ_ENTRY(compress),
     TQ_ENTRY(compress_device_params), TQ_ENTRY(decompress_aggregate), TQ_ENTRY(decompress_aggregate_rows), TQ_ENTRY(decompress_aggregate_apply),
     TQ_ENTRY(decompress_aggregate_device_params), TQ_ENTRY(stats_segments), TQ_ENTRY(stats_hinted_segments), TQ_ENTRY(compress_segments),
