@@ -423,11 +423,35 @@ class MxMatrix:
     """A [rows, cols] matrix of E2M1 codes with an E8M0 scale for every 32 elements of a row (tq_mx_t, include/tq.h).
 
     ``codes`` is a uint8 tensor [rows, >= 16 * ceil(cols / 32)]; ``scales`` a uint8 tensor of ceil(rows / 128) rows (MX_TILES) or
-    ``rows`` rows (MX_ROWS).  Both may be views with any row stride that is a multiple of 16 bytes."""
-    __slots__ = ("codes", "scales", "rows", "cols", "layout")
+    ``rows`` rows (MX_ROWS).  Both may be views with any row stride that is a multiple of 16 bytes.  The matrices that the calls
+    return hold both in one piece, ``memory``, of which ``codes`` and ``scales`` are views."""
+    __slots__ = ("_codes", "_scales", "rows", "cols", "layout", "memory")
 
-    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, layout: int = MX_TILES):
-        self.codes, self.scales, self.rows, self.cols, self.layout = codes, scales, rows, cols, layout
+    def __init__(self, codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], rows: int, cols: int, layout: int = MX_TILES,
+                 memory: Optional[torch.Tensor] = None):
+        self._codes, self._scales, self.rows, self.cols, self.layout, self.memory = codes, scales, rows, cols, layout, memory
+
+    def _views(self):
+        width, stride, at, scale_rows, scale_stride = _calls().mx_layout(self.rows, self.cols, self.layout)
+        self._codes = self.memory[:self.rows * stride].view(self.rows, stride)[:, :width]
+        self._scales = self.memory[at:at + scale_rows * scale_stride].view(scale_rows, scale_stride)
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            self._views()
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            self._views()
+        return self._scales
+
+    @property
+    def like(self) -> torch.Tensor:
+        """A tensor on the matrix's device."""
+        return self._codes if self.memory is None else self.memory
 
 
 def tq_mx_code_stride(cols: int) -> int:
@@ -440,9 +464,11 @@ def tq_mx_scale_stride(cols: int, layout: int = MX_TILES) -> int:
 
 def new_mx(rows: int, cols: int, layout: int = MX_TILES, device="cuda") -> MxMatrix:
     """Memory for a matrix, uninitialised; the calls that write one write all of it, the filling of its last scale tiles included."""
-    index = device.index if isinstance(device, torch.device) else torch.device(device).index
-    codes, scales = _calls().new_mx(rows, cols, layout, torch.cuda.current_device() if index is None else index)
-    return MxMatrix(codes, scales, rows, cols, layout)
+    return _new_mx(torch.empty(0, dtype=torch.uint8, device=device), rows, cols, layout)
+
+
+def _new_mx(like: torch.Tensor, rows: int, cols: int, layout: int) -> MxMatrix:
+    return MxMatrix(None, None, rows, cols, layout, _calls().new_mx(like, rows, cols, layout))
 
 
 def _new_plain(like: torch.Tensor, rows: Optional[int], cols: int, dtype: torch.dtype) -> torch.Tensor:
@@ -459,7 +485,7 @@ def tq_mx_quantize(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int = 0, f
                    layout: int = MX_TILES, out: Optional[MxMatrix] = None, stream=None) -> MxMatrix:
     """Enqueue the quantisation of ``x`` ([rows, cols] or [cols], fp32 or bf16) along its rows; the first ``cols`` columns when given."""
     if out is None:
-        out = new_mx(_rows(x), x.shape[-1] if cols is None else cols, layout, x.device)
+        out = _new_mx(x, _rows(x), x.size(-1) if cols is None else cols, layout)
     _check(_calls().mx_quantize(x, rounding, _seed(seed), first_row, out, stream), "tq_mx_quantize")
     return out
 
@@ -468,9 +494,9 @@ def tq_mx_quantize_both(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int =
                         out_t: Optional[MxMatrix] = None, stream=None) -> Tuple[MxMatrix, MxMatrix]:
     """``x`` along its rows, and its transposed copy, whose blocks run along x's columns."""
     if out is None:
-        out = new_mx(_rows(x), x.shape[-1], MX_TILES, x.device)
+        out = _new_mx(x, _rows(x), x.size(-1), MX_TILES)
     if out_t is None:
-        out_t = new_mx(out.cols, out.rows, MX_TILES, x.device)
+        out_t = _new_mx(x, out.cols, out.rows, MX_TILES)
     _check(_calls().mx_quantize_both(x, rounding, _seed(seed), first_row, out, out_t, stream), "tq_mx_quantize_both")
     return out, out_t
 
@@ -478,7 +504,7 @@ def tq_mx_quantize_both(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int =
 def tq_mx_dequantize(m: MxMatrix, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The values of ``m`` as a [rows, cols] tensor."""
     if out is None:
-        out = _new_plain(m.codes, m.rows, m.cols, dtype)
+        out = _new_plain(m.like, m.rows, m.cols, dtype)
     _check(_calls().mx_dequantize(m, out, stream), "tq_mx_dequantize")
     return out
 
@@ -486,7 +512,7 @@ def tq_mx_dequantize(m: MxMatrix, dtype: torch.dtype = torch.float32, out: Optio
 def tq_mx_decompress_aggregate(m: MxMatrix, weights: Optional[Sequence[float]] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue the mean (or weighted sum) of the rows of ``m`` (layout MX_ROWS); returns the [cols] fp32 update."""
     if out is None:
-        out = _new_plain(m.codes, None, m.cols, torch.float32)
+        out = _new_plain(m.like, None, m.cols, torch.float32)
     _check(_calls().mx_decompress_aggregate(m, weights, out, stream), "tq_mx_decompress_aggregate")
     return out
 
@@ -494,7 +520,7 @@ def tq_mx_decompress_aggregate(m: MxMatrix, weights: Optional[Sequence[float]] =
 def tq_mx_product(a: MxMatrix, b: MxMatrix, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue a b^T; returns [a.rows, b.rows]."""
     if out is None:
-        out = _new_plain(a.codes, a.rows, b.rows, dtype)
+        out = _new_plain(a.like, a.rows, b.rows, dtype)
     _check(_calls().mx_product(a, b, out, stream), "tq_mx_product")
     return out
 
@@ -504,7 +530,7 @@ def tq_mx_gated(x: MxMatrix, w_gate: MxMatrix, w_up: MxMatrix, activation: int =
     """Enqueue act(x w_gate^T) * (x w_up^T), quantised along its rows.  ``projections``: a [tokens, 2 features] tensor that receives both
     projections, for tq_mx_gated_backward."""
     if out is None:
-        out = new_mx(x.rows, w_gate.rows, MX_TILES, x.codes.device)
+        out = _new_mx(x.like, x.rows, w_gate.rows, MX_TILES)
     _check(_calls().mx_gated(x, w_gate, w_up, activation, out, projections, stream), "tq_mx_gated")
     return out
 
@@ -515,11 +541,11 @@ def tq_mx_gated_backward(dh: torch.Tensor, projections: torch.Tensor, activation
     """Enqueue the backward pass of tq_mx_gated up to the products; returns ([dg | du], its transposed copy, the transposed h)."""
     tokens, features = _rows(dh), dh.shape[-1]
     if dgu is None:
-        dgu = new_mx(tokens, 2 * features, MX_TILES, dh.device)
+        dgu = _new_mx(dh, tokens, 2 * features, MX_TILES)
     if dgu_t is None:
-        dgu_t = new_mx(2 * features, tokens, MX_TILES, dh.device)
+        dgu_t = _new_mx(dh, 2 * features, tokens, MX_TILES)
     if h_t is None:
-        h_t = new_mx(features, tokens, MX_TILES, dh.device)
+        h_t = _new_mx(dh, features, tokens, MX_TILES)
     _check(_calls().mx_gated_backward(dh, projections, activation, rounding, _seed(seed), dgu, dgu_t, h_t, stream), "tq_mx_gated_backward")
     return dgu, dgu_t, h_t
 

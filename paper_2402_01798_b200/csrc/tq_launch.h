@@ -73,6 +73,18 @@ inline int sm_count() {
     return sms;
 }
 
+// Lets a kernel have more than 48 KB of shared memory: once for each kernel and device, up to `most`.
+template <class K>
+inline cudaError_t allow_shared_memory(K* kernel, size_t most, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    if (const cudaError_t e = cudaGetDevice(&dev)) return e;
+    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (bit & done.load(std::memory_order_relaxed)) return cudaSuccess;
+    if (const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most))) return e;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
 // Every kernel is launched through this: it may be set up (blocks placed, barriers initialised, tables built from kernel
 // parameters) while the kernel before it on the stream is still running, and waits for that one's results at its
 // pdl_wait().  Without it each launch of a round's chain begins about 1 us after the end of the one before it.

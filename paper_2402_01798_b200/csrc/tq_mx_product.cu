@@ -140,10 +140,6 @@ struct ProductArgs {
     MxView h;                                                    // gated only
 };
 
-__device__ __forceinline__ void stg256_words(void* p, const uint32_t (&v)[8]) {
-    asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
-                 :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "l"(p) : "memory");
-}
 // WIDTH consecutive elements of 32 rows, one row a thread: `row0` is the warp's first.  Where rows start on 16-byte boundaries and all columns exist
 // a thread stores its row; else eight columns at a time change places in `scratch` (the warp's 32 x 9 words), so that eight threads
 // store neighbours (32 scattered elements a store took 47 us for 300 x 300 x 8192).
@@ -764,9 +760,11 @@ ProductPlan plan_product(uint32_t m, uint32_t n, uint32_t k, uint32_t a_rows) {
     return plan;
 }
 
-template <class K>
-cudaError_t launch_clustered(K* kernel, unsigned blocks, unsigned cluster, unsigned threads, size_t smem, cudaStream_t stream, void** args) {
-    if (const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))) return e;
+// `most`: of shared memory, for any call
+template <auto KERNEL>
+cudaError_t launch_clustered(unsigned blocks, unsigned cluster, unsigned threads, size_t smem, size_t most, cudaStream_t stream, void** args) {
+    static std::atomic<uint64_t> allowed{0};
+    if (const cudaError_t e = allow_shared_memory(KERNEL, most, allowed)) return e;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -774,7 +772,7 @@ cudaError_t launch_clustered(K* kernel, unsigned blocks, unsigned cluster, unsig
     attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = cluster ? 2 : 1;
-    return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kernel), args);
+    return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(KERNEL), args);
 }
 
 // Scale tiles, two at a time.
@@ -790,9 +788,10 @@ cudaError_t scales_map(CUtensorMap* map, const tq_mx_t& m) {
 
 template <int GATED, int SPLIT>
 cudaError_t launch_split_as(const CUtensorMap& map_a, const CUtensorMap& map_b0, const CUtensorMap& map_b1, const ProductArgs& p, cudaStream_t stream) {
+    using S = SplitShape<GATED>;
     SplitMemory mem = split_memory<GATED>(p.m < 128 ? p.m : 128, p.a_rows, (static_cast<uint64_t>(p.k) + kBK - 1) / kBK, SPLIT);
     void* args[] = {const_cast<CUtensorMap*>(&map_a), const_cast<CUtensorMap*>(&map_b0), const_cast<CUtensorMap*>(&map_b1), const_cast<ProductArgs*>(&p), &mem.stages, &mem.stage_bytes};
-    return launch_clustered(mx_split_kernel<GATED, SPLIT>, p.tiles_m * p.tiles_n * SPLIT, SPLIT, kSplitThreads, mem.bytes, stream, args);
+    return launch_clustered<mx_split_kernel<GATED, SPLIT>>(p.tiles_m * p.tiles_n * SPLIT, SPLIT, kSplitThreads, mem.bytes, S::kMostStageSmem + 2048, stream, args);
 }
 
 template <int GATED>
@@ -822,7 +821,7 @@ cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t
         if (const cudaError_t e = scales_map(&maps.b0, b0)) return e;
         if (const cudaError_t e = scales_map(&maps.b1, b1)) return e;
         void* args[] = {&map_a, &map_b0, &map_b1, &maps, &p};
-        return launch_clustered(mx_pair_kernel<GATED>, 2 * (tiles < pairs ? tiles : pairs), 0, kPairThreads, kPairSmem, stream, args);
+        return launch_clustered<mx_pair_kernel<GATED>>(2 * (tiles < pairs ? tiles : pairs), 0, kPairThreads, kPairSmem, kPairSmem, stream, args);
     }
     p.tiles_m = (p.m + 127) / 128; p.tiles_n = (p.n + 127) / 128;
     if (plan.split == 2) return launch_split_as<GATED, 2>(map_a, map_b0, map_b1, p, stream);

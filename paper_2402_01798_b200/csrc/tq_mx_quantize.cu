@@ -200,65 +200,145 @@ __global__ void __launch_bounds__(kThreads, 4) mx_tile_kernel(MxInput in, MxView
 }
 
 // ---- decoding ----------------------------------------------------------------------------------------------------
-// A thread makes 8 elements in each of 4 rows.  WIDE: it stores them in one piece; else the warp passes its codes around so that consecutive threads
-// store consecutive elements, for rows on any boundary.  A block covers 8 << shift columns and 4 * (256 >> shift) rows.
-constexpr int kDecodeRows = 4;
-template <bool BF16, bool WIDE>
-__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxView m, void* out, uint64_t stride, uint32_t chunks, uint32_t shift) {
+// Row and column of this thread, which makes EACH elements in each of ROWS rows: a block covers EACH << shift columns and ROWS * (256 >> shift) rows.
+template <int EACH, int ROWS>
+struct DecodePlace {
+    uint32_t high, row;
+    uint64_t col;
+    __device__ __forceinline__ DecodePlace(uint32_t chunks, uint32_t shift) {
+        high = kThreads >> shift;
+        row = blockIdx.x / chunks * (high * ROWS) + (threadIdx.x >> shift);
+        col = (static_cast<uint64_t>(blockIdx.x % chunks) * EACH << shift) + (threadIdx.x & ((1u << shift) - 1)) * EACH;
+    }
+};
+__device__ __forceinline__ uint64_t mx_scale_row(const MxView& m, uint32_t row) {              // where row's first scale is
+    return m.tiles ? (row >> 7) * m.scale_stride + (row & 31) * 16 + ((row >> 5) & 3) * 4 : row * m.scale_stride;
+}
+
+// Rows that start on 16-byte boundaries (`wide`: 32): 16 elements of 2 rows, stored in pieces of 32 or 16 bytes.
+constexpr int kWideEach = 16, kWideRows = 2;
+template <bool BF16>
+__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxView m, void* out, uint64_t stride, uint32_t chunks, uint32_t shift, uint32_t wide) {
     pdl_wait();
-    const uint32_t high = kThreads >> shift;
-    const uint64_t row0 = static_cast<uint64_t>(blockIdx.x / chunks) * (high * kDecodeRows) + (threadIdx.x >> shift);
-    const uint64_t col = (static_cast<uint64_t>(blockIdx.x % chunks) << (shift + 3)) + (threadIdx.x & ((1u << shift) - 1)) * 8;
-    const bool any = col < m.cols;
-    uint32_t codes[kDecodeRows], byte[kDecodeRows];
+    const DecodePlace<kWideEach, kWideRows> at(chunks, shift);
+    if (at.col >= m.cols) return;
+    const uint64_t scale_at = m.tiles ? (at.col >> 7) * 512 + ((at.col >> 5) & 3) : at.col >> 5;
+    uint32_t codes[kWideRows][2], byte[kWideRows];
 #pragma unroll
-    for (int i = 0; i < kDecodeRows; ++i) {
-        const uint64_t row = row0 + i * high;
-        codes[i] = byte[i] = 0;
-        if (any && row < m.rows) {
-            asm volatile("ld.global.b32 %0, [%1];" : "=r"(codes[i]) : "l"(m.codes + row * m.code_stride + col / 2) : "memory");
-            byte[i] = ldg8(m.scales + mx_scale_at(m, row, col / 32));
+    for (int i = 0; i < kWideRows; ++i) {
+        const uint32_t row = at.row + i * at.high;
+        codes[i][0] = codes[i][1] = byte[i] = 0;
+        if (row < m.rows) {
+            asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(codes[i][0]), "=r"(codes[i][1]) : "l"(m.codes + row * m.code_stride + at.col / 2) : "memory");
+            byte[i] = ldg8(m.scales + mx_scale_row(m, row) + scale_at);
         }
     }
-    char* to = static_cast<char*>(out) + row0 * stride * (BF16 ? 2 : 4);
 #pragma unroll
-    for (int i = 0; i < kDecodeRows; ++i, to += high * stride * (BF16 ? 2 : 4)) {
-        if (row0 + i * high >= m.rows) continue;                 // a whole warp's, where warps exchange codes
-        const float scale = mx_scale_value(byte[i]);
-        if constexpr (WIDE) {
-            float v[8];
-            e2m1_values8(codes[i], v);
+    for (int i = 0; i < kWideRows; ++i) {
+        const uint32_t row = at.row + i * at.high;
+        if (row >= m.rows) continue;
+        char* const to = static_cast<char*>(out) + (row * stride + at.col) * (BF16 ? 2 : 4);
+        const f32x2 scale = both(mx_scale_value(byte[i]));
+        float v[16];
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) unpair(mul2(pair(v[e], v[e + 1]), both(scale)), v[e], v[e + 1]);
-            if (col + 8 <= m.cols) {
-                if constexpr (BF16) {
-                    stg128(to + col * 2, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
-                } else {
-                    stg128(to + col * 4, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
-                    stg128(to + col * 4 + 16, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
-                }
+        for (int q = 0; q < 2; ++q) {
+            float x[8];
+            e2m1_values8(codes[i][q], x);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) unpair(mul2(pair(x[e], x[e + 1]), scale), v[8 * q + e], v[8 * q + e + 1]);
+        }
+        if (at.col + kWideEach <= m.cols) {
+            if constexpr (BF16) {
+                uint32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                if (wide == 32) stg256_words(to, w);
+                else { stg128(to, make_uint4(w[0], w[1], w[2], w[3])); stg128(to + 16, make_uint4(w[4], w[5], w[6], w[7])); }
             } else {
+                uint32_t w[16];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (col + e < m.cols) {
-                        if constexpr (BF16) reinterpret_cast<unsigned short*>(to)[col + e] = static_cast<unsigned short>(__float_as_uint(v[e]) >> 16);   // exact
-                        else reinterpret_cast<float*>(to)[col + e] = v[e];
-                    }
+                for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(v[e]);
+                if (wide == 32) {
+                    const uint32_t lo[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]}, hi[8] = {w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]};
+                    stg256_words(to, lo);
+                    stg256_words(to + 32, hi);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) stg128(to + 16 * e, make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]));
+                }
             }
-        } else {                                                 // shift >= 5: a warp lies in one row
-            const uint32_t lane = threadIdx.x & 31;
-            const uint64_t first = col - lane * 8;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (at.col + e < m.cols) {
+                    if constexpr (BF16) reinterpret_cast<unsigned short*>(to)[e] = static_cast<unsigned short>(__float_as_uint(v[e]) >> 16);   // exact
+                    else reinterpret_cast<float*>(to)[e] = v[e];
+                }
+        }
+    }
+}
+
+// Rows on any boundary: 8 elements of 4 rows; a warp's 256 go through shared memory, so that consecutive threads store consecutive words.  bf16 rows may
+// start in the middle of a word: two elements a thread all the same, the first and last alone.
+constexpr int kRaggedEach = 8, kRaggedRows = 4;
+template <bool BF16>
+__global__ void __launch_bounds__(kThreads) mx_dequantize_ragged_kernel(MxView m, void* out, uint64_t stride, uint32_t chunks, uint32_t shift) {
+    constexpr int kWords = BF16 ? 128 : 256;
+    __shared__ __align__(16) uint32_t staged[kThreads / 32][kWords];
+    pdl_wait();
+    const DecodePlace<kRaggedEach, kRaggedRows> at(chunks, shift);
+    const uint32_t lane = threadIdx.x & 31;
+    uint32_t* const words = staged[threadIdx.x / 32];
+    const uint64_t first = at.col - lane * kRaggedEach;          // shift >= 5: a warp lies in one row
+    if (first >= m.cols) return;
+    const bool any = at.col < m.cols;
+    const int count = m.cols - first < 256 ? static_cast<int>(m.cols - first) : 256;
+    const uint64_t scale_at = m.tiles ? (at.col >> 7) * 512 + ((at.col >> 5) & 3) : at.col >> 5;
+    uint32_t codes[kRaggedRows], byte[kRaggedRows];
+#pragma unroll
+    for (int i = 0; i < kRaggedRows; ++i) {
+        const uint32_t row = at.row + i * at.high;
+        codes[i] = byte[i] = 0;
+        if (any && row < m.rows) {
+            asm volatile("ld.global.b32 %0, [%1];" : "=r"(codes[i]) : "l"(m.codes + row * m.code_stride + at.col / 2) : "memory");
+            byte[i] = ldg8(m.scales + mx_scale_row(m, row) + scale_at);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kRaggedRows; ++i) {
+        const uint32_t row = at.row + i * at.high;
+        if (row >= m.rows) break;                                // a whole warp's
+        const f32x2 scale = both(mx_scale_value(byte[i]));
+        float v[8];
+        e2m1_values8(codes[i], v);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) unpair(mul2(pair(v[e], v[e + 1]), scale), v[e], v[e + 1]);
+        __syncwarp();
+        if constexpr (BF16) {
+            *reinterpret_cast<uint4*>(&words[4 * lane]) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            __syncwarp();
+            unsigned short* const to = static_cast<unsigned short*>(out) + row * stride + first;
+            const int off = static_cast<int>(reinterpret_cast<uintptr_t>(to) >> 1 & 1);
+#pragma unroll
+            for (int k = 0; k < 5; ++k) {
+                const int t = 32 * k + static_cast<int>(lane), e = 2 * t - off;          // elements e and e + 1
+                if (k == 4 && (lane != 0 || off == 0)) break;
+                const uint32_t here = t < 128 ? words[t] : 0u, before = off && t > 0 ? words[t - 1] : 0u;
+                const uint32_t two = off ? __byte_perm(before, here, 0x5432) : here;
+                if (e >= 0 && e + 1 < count) asm volatile("st.global.b32 [%0], %1;" ::"l"(to + e), "r"(two) : "memory");
+                else if (e >= 0 && e < count) to[e] = static_cast<unsigned short>(two);
+                else if (e == -1 && count > 0) to[0] = static_cast<unsigned short>(two >> 16);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                *reinterpret_cast<float4*>(&words[8 * lane + 4 * q]) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+            __syncwarp();
+            float* const to = static_cast<float*>(out) + row * stride + first;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const uint32_t w = __shfl_sync(0xFFFFFFFFu, codes[i], 4 * k + lane / 8);
-                const float s = __shfl_sync(0xFFFFFFFFu, scale, 4 * k + lane / 8);
-                float v[8];
-                e2m1_values8(w >> (4 * (lane & 7)), v);
-                const uint64_t c = first + 32 * k + lane;
-                if (c < m.cols) {
-                    if constexpr (BF16) reinterpret_cast<unsigned short*>(to)[c] = static_cast<unsigned short>(__float_as_uint(v[0] * s) >> 16);
-                    else reinterpret_cast<float*>(to)[c] = v[0] * s;
-                }
+                const int e = 32 * k + static_cast<int>(lane);
+                if (e < count) to[e] = __uint_as_float(words[e]);
             }
         }
     }
@@ -268,10 +348,33 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxView m, void*
 struct MxWeights {
     float w[TQ_MAX_WORKERS];
 };
+// Eight sums over n, each rounded once.  inv = 1 / n rounded; for a power of two the product is all there is to it.  Else one step of Markstein's (IBM J. Res. Dev. 34,
+// 1990): with q = x inv, the remainder x - q n is exact in a fused operation, and q + remainder * inv is x / n correctly rounded as long as nothing
+// underflows.  Tiny sums, infinities and NaN take the division itself (for all, 2 rows of 50 M took 140 us instead of 54).
+__device__ __forceinline__ void divide8(float (&v)[8], float n, float inv, bool exact) {
+    if (exact) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= inv;
+        return;
+    }
+    bool plain = true;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) plain = plain && ((__float_as_uint(v[e]) & 0x7FFFFFFFu) - 0x10000000u < 0x6F800000u || v[e] == 0.0f);      // 2^-95 <= |x| < infinity
+    if (plain) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float q = v[e] * inv;
+            v[e] = fmaf(fmaf(-q, n, v[e]), inv, q);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __fdiv_rn(v[e], n);
+    }
+}
 // A thread decodes the same EACH elements of every worker's row (32, a block; 8 where the rows are too short to fill the GPU so) and keeps their sums.
 // fp32, in worker order; code * scale is exact, so that one fused operation adds it.
 template <bool WEIGHTED, int EACH>
-__global__ void __launch_bounds__(kThreads) mx_aggregate_kernel(MxView m, float* out, uint32_t n, float divisor, MxWeights weights) {
+__global__ void __launch_bounds__(kThreads) mx_aggregate_kernel(MxView m, float* out, uint32_t n, float divisor, float inv, bool exact, MxWeights weights) {
     pdl_wait();
     const uint64_t first = (static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x) * EACH;
     if (first >= m.cols) return;
@@ -280,25 +383,37 @@ __global__ void __launch_bounds__(kThreads) mx_aggregate_kernel(MxView m, float*
     for (int e = 0; e < EACH / 2; ++e) sum[e] = both(0.0f);
     const uint8_t* codes = m.codes + first / 2;
     const uint8_t* scales = m.scales + first / 32;
-#pragma unroll 4
-    for (uint32_t i = 0; i < n; ++i, codes += m.code_stride, scales += m.scale_stride) {
-        uint32_t w[EACH / 8];
-        if constexpr (EACH == 32) {
-            const uint4 c = ldg128(codes);
-            w[0] = c.x; w[1] = c.y; w[2] = c.z; w[3] = c.w;
-        } else {
-            asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(codes) : "memory");
+    constexpr uint32_t kAhead = EACH == 8 ? 16 : 4;          // workers whose codes are asked for at a time
+#pragma unroll 1
+    for (uint32_t i0 = 0; i0 < n; i0 += kAhead) {
+        uint32_t w[kAhead][EACH / 8], byte[kAhead];
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) {
+            if (i0 + i < n) {
+                if constexpr (EACH == 32) {
+                    const uint4 c = ldg128(codes);
+                    w[i][0] = c.x; w[i][1] = c.y; w[i][2] = c.z; w[i][3] = c.w;
+                } else {
+                    asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[i][0]) : "l"(codes) : "memory");
+                }
+                byte[i] = ldg8(scales);
+            }
+            codes += m.code_stride; scales += m.scale_stride;
         }
-        const f32x2 scale = both(mx_scale_value(ldg8(scales)));
 #pragma unroll
-        for (int q = 0; q < EACH / 8; ++q) {
-            float v[8];
-            e2m1_values8(w[q], v);
+        for (uint32_t i = 0; i < kAhead; ++i) {
+            if (i0 + i >= n) break;
+            const f32x2 scale = both(mx_scale_value(byte[i]));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                f32x2& to = sum[4 * q + e];
-                if constexpr (WEIGHTED) to = add2(to, mul2(mul2(pair(v[2 * e], v[2 * e + 1]), scale), both(weights.w[i])));
-                else to = fma2(pair(v[2 * e], v[2 * e + 1]), scale, to);
+            for (int q = 0; q < EACH / 8; ++q) {
+                float v[8];
+                e2m1_values8(w[i][q], v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f32x2& to = sum[4 * q + e];
+                    if constexpr (WEIGHTED) to = add2(to, mul2(mul2(pair(v[2 * e], v[2 * e + 1]), scale), both(weights.w[i0 + i])));
+                    else to = fma2(pair(v[2 * e], v[2 * e + 1]), scale, to);
+                }
             }
         }
     }
@@ -308,8 +423,8 @@ __global__ void __launch_bounds__(kThreads) mx_aggregate_kernel(MxView m, float*
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             unpair(sum[4 * q + e], v[2 * e], v[2 * e + 1]);
-            if constexpr (!WEIGHTED) { v[2 * e] = __fdiv_rn(v[2 * e], divisor); v[2 * e + 1] = __fdiv_rn(v[2 * e + 1], divisor); }
         }
+        if constexpr (!WEIGHTED) divide8(v, divisor, inv, exact);
         const uint64_t col = first + 8 * q;
         if (col + 8 <= m.cols) stg256(out + col, v);
         else
@@ -375,12 +490,14 @@ __global__ void __launch_bounds__(kThreads, 2) mx_gated_backward_kernel(MxGatedI
     encode_col<false>(t, h_t, c0, r0, height, width, last);
 }
 
-template <class K>
-cudaError_t allow_smem(K* kernel, size_t bytes) {
-    return cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-}
-
 uint32_t boundary(uint64_t at) { return at % 32 == 0 ? 32 : at % 16 == 0 ? 16 : 0; }
+
+template <auto KERNEL, class... A>
+cudaError_t launch_tiled(dim3 grid, size_t smem, cudaStream_t stream, const A&... args) {
+    static std::atomic<uint64_t> allowed{0};
+    if (const cudaError_t e = allow_shared_memory(KERNEL, smem, allowed)) return e;
+    return launch_kernel(KERNEL, grid, kThreads, smem, stream, args...);
+}
 
 template <bool BF16, bool STOCHASTIC>
 cudaError_t launch_quantize_as(const MxQuantizeCall& c) {
@@ -398,12 +515,8 @@ cudaError_t launch_quantize_as(const MxQuantizeCall& c) {
     }
     const uint64_t across = (cols + kTileCols - 1) / kTileCols, down = (rows + 127) / 128 * 2;       // whole scale tiles
     const dim3 grid(static_cast<unsigned>(across * down));
-    if (c.out_t) {
-        if (const cudaError_t e = allow_smem(mx_tile_kernel<BF16, STOCHASTIC, true>, tile_bytes(STOCHASTIC))) return e;
-        return launch_kernel(mx_tile_kernel<BF16, STOCHASTIC, true>, grid, kThreads, tile_bytes(STOCHASTIC), c.stream, in, out, out_t, static_cast<uint32_t>(across), keys, c.first_row);
-    }
-    if (const cudaError_t e = allow_smem(mx_tile_kernel<BF16, STOCHASTIC, false>, tile_bytes(STOCHASTIC))) return e;
-    return launch_kernel(mx_tile_kernel<BF16, STOCHASTIC, false>, grid, kThreads, tile_bytes(STOCHASTIC), c.stream, in, out, out_t, static_cast<uint32_t>(across), keys, c.first_row);
+    if (c.out_t) return launch_tiled<mx_tile_kernel<BF16, STOCHASTIC, true>>(grid, tile_bytes(STOCHASTIC), c.stream, in, out, out_t, static_cast<uint32_t>(across), keys, c.first_row);
+    return launch_tiled<mx_tile_kernel<BF16, STOCHASTIC, false>>(grid, tile_bytes(STOCHASTIC), c.stream, in, out, out_t, static_cast<uint32_t>(across), keys, c.first_row);
 }
 
 template <bool BF16, bool GELU, bool STOCHASTIC>
@@ -412,9 +525,7 @@ cudaError_t launch_gated_backward_as(const MxGatedBackwardCall& c) {
     const uint64_t size = BF16 ? 2 : 4;
     const MxGatedInput in{c.dh, c.gu, c.dh_stride, c.gu_stride, features,
                           boundary(reinterpret_cast<uintptr_t>(c.dh) | reinterpret_cast<uintptr_t>(c.gu) | (c.dgu->rows > 1 ? (c.dh_stride | c.gu_stride) * size : 0))};
-    auto* kernel = mx_gated_backward_kernel<BF16, GELU, STOCHASTIC>;
-    if (const cudaError_t e = allow_smem(kernel, tile_bytes(STOCHASTIC))) return e;
-    return launch_kernel(kernel, dim3(static_cast<unsigned>(across * down)), kThreads, tile_bytes(STOCHASTIC), c.stream, in, mx_view(*c.dgu), mx_view(*c.dgu_t), mx_view(*c.h_t),
+    return launch_tiled<mx_gated_backward_kernel<BF16, GELU, STOCHASTIC>>(dim3(static_cast<unsigned>(across * down)), tile_bytes(STOCHASTIC), c.stream, in, mx_view(*c.dgu), mx_view(*c.dgu_t), mx_view(*c.h_t),
                          static_cast<uint32_t>(across), round_keys(c.seed));
 }
 template <bool BF16, bool GELU>
@@ -430,14 +541,14 @@ cudaError_t launch_mx_quantize(const MxQuantizeCall& c) {
 }
 
 cudaError_t launch_mx_dequantize(const tq_mx_t& m, void* out, bool bf16, uint64_t stride, cudaStream_t stream) {
-    const bool wide = (reinterpret_cast<uintptr_t>(out) | (m.rows > 1 ? stride * (bf16 ? 2 : 4) : 0)) % 16 == 0;
-    uint32_t shift = wide ? 2 : 5;
-    while (shift < 8 && (8ull << shift) < m.cols) ++shift;
-    const uint64_t chunks = (m.cols + (8ull << shift) - 1) >> (shift + 3), high = static_cast<uint64_t>(kThreads >> shift) * kDecodeRows;
+    const uint32_t wide = boundary(reinterpret_cast<uintptr_t>(out) | (m.rows > 1 ? stride * (bf16 ? 2 : 4) : 0));
+    const uint64_t each = wide ? kWideEach : kRaggedEach;
+    uint32_t shift = wide ? 1 : 5;
+    while (shift < 8 && (each << shift) < m.cols) ++shift;
+    const uint64_t chunks = (m.cols + (each << shift) - 1) / (each << shift), high = static_cast<uint64_t>(kThreads >> shift) * (wide ? kWideRows : kRaggedRows);
     const dim3 grid(static_cast<unsigned>(chunks * ((m.rows + high - 1) / high)));
-    auto* kernel = bf16 ? (wide ? mx_dequantize_kernel<true, true> : mx_dequantize_kernel<true, false>)
-                        : (wide ? mx_dequantize_kernel<false, true> : mx_dequantize_kernel<false, false>);
-    return launch_kernel(kernel, grid, kThreads, 0, stream, mx_view(m), out, stride, static_cast<uint32_t>(chunks), shift);
+    if (wide) return launch_kernel(bf16 ? mx_dequantize_kernel<true> : mx_dequantize_kernel<false>, grid, kThreads, 0, stream, mx_view(m), out, stride, static_cast<uint32_t>(chunks), shift, wide);
+    return launch_kernel(bf16 ? mx_dequantize_ragged_kernel<true> : mx_dequantize_ragged_kernel<false>, grid, kThreads, 0, stream, mx_view(m), out, stride, static_cast<uint32_t>(chunks), shift);
 }
 
 cudaError_t launch_mx_aggregate(const tq_mx_t& m, const float* weights, float* out, cudaStream_t stream) {
@@ -450,7 +561,7 @@ cudaError_t launch_mx_aggregate(const tq_mx_t& m, const float* weights, float* o
     const dim3 grid(static_cast<unsigned>((m.cols + each * kThreads - 1) / (each * kThreads)));
     auto* kernel = shortened ? (weights ? mx_aggregate_kernel<true, 8> : mx_aggregate_kernel<false, 8>)
                              : (weights ? mx_aggregate_kernel<true, 32> : mx_aggregate_kernel<false, 32>);
-    return launch_kernel(kernel, grid, kThreads, 0, stream, mx_view(m), out, n, static_cast<float>(n), w);
+    return launch_kernel(kernel, grid, kThreads, 0, stream, mx_view(m), out, n, static_cast<float>(n), 1.0f / static_cast<float>(n), (n & (n - 1)) == 0, w);
 }
 
 cudaError_t launch_mx_gated_backward(const MxGatedBackwardCall& c) {

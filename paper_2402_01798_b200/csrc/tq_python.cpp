@@ -4,7 +4,7 @@
 // 2.6 us of the launch, which bounds rounds of short gradients.
 #include <Python.h>
 
-#include <ATen/ops/as_strided.h>
+#include <ATen/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -381,10 +381,26 @@ tq_status decompress_aggregate_segments(Args& a) {           // packed, segments
                                            a.stream());
 }
 
-// ---- microscaled 4-bit floating point: an MxMatrix (binding.py) is five attributes --------------------------------
+// ---- microscaled 4-bit floating point: an MxMatrix (binding.py) is six attributes ---------------------------------
 struct MxNames {
-    PyObject *codes, *scales, *rows, *cols, *layout;
+    PyObject *codes, *scales, *rows, *cols, *layout, *memory;
 } N;
+// A matrix in one piece of memory: codes, and on the next 128-byte boundary scales.  Rows of codes that are longer than 128 bytes start on such a
+// boundary: the products load 128 bytes of a row at a time.
+struct MxPlace {
+    uint64_t width, stride, scales, scale_rows, scale_stride, bytes;
+};
+MxPlace mx_place(uint64_t rows, uint64_t cols, bool tiles) {
+    MxPlace p;
+    const uint64_t blocks = (cols + 31) / 32;
+    p.width = blocks * 16;
+    p.stride = p.width > 128 ? (p.width + 127) / 128 * 128 : p.width;
+    p.scales = (rows * p.stride + 127) / 128 * 128;
+    p.scale_rows = tiles ? (rows + 127) / 128 : rows;
+    p.scale_stride = tiles ? (blocks + 3) / 4 * 512 : (blocks + 15) / 16 * 16;
+    p.bytes = p.scales + p.scale_rows * p.scale_stride;
+    return p;
+}
 
 // Kernels run on the current device and take addresses of no other.
 void on_current_device(const at::Tensor& t, const char* what) {
@@ -417,6 +433,20 @@ tq_mx_t mx(Args& a) {
     tq_mx_t m{};
     m.rows = attribute(o, N.rows); m.cols = attribute(o, N.cols);
     m.layout = static_cast<uint32_t>(attribute(o, N.layout));
+    PyObject* memory = PyObject_GetAttr(o, N.memory);
+    if (!memory) throw Failed();
+    Py_DECREF(memory);                                             // held by the matrix
+    if (memory != Py_None) {
+        if (!THPVariable_Check(memory)) fail(PyExc_TypeError, "a matrix's memory must be a tensor");
+        const at::Tensor& t = THPVariable_Unpack(memory);
+        on_current_device(t, "matrix");
+        if (m.rows >= (1ull << 31) || m.cols > (1ull << 40)) return m;                       // the library refuses it
+        const MxPlace p = mx_place(m.rows, m.cols, m.layout == TQ_MX_TILES);
+        if (t.scalar_type() != at::kByte || !t.is_contiguous() || static_cast<uint64_t>(t.numel()) < p.bytes) fail(PyExc_ValueError, "the memory is smaller than the matrix");
+        m.codes = static_cast<uint8_t*>(t.data_ptr()); m.scales = m.codes + p.scales;
+        m.code_stride = p.stride; m.scale_stride = p.scale_stride;
+        return m;
+    }
     const uint64_t blocks = m.cols / 32 + (m.cols % 32 != 0);
     const bool tiles = m.layout == TQ_MX_TILES;
     m.codes = bytes_of(o, N.codes, "codes", m.rows, blocks * 16, &m.code_stride);
@@ -444,6 +474,13 @@ Plain plain(const at::Tensor& t, const char* what, uint64_t rows, uint64_t cols)
     p.stride = have > 1 ? static_cast<uint64_t>(t.stride(0)) : wide;
     return p;
 }
+// Memory from torch's allocator, as torch.empty takes it but straight: through the dispatcher a matrix costs 1.9 us of host time.  On the current device, where
+// the kernels run; a tensor for another one comes from at::empty.
+at::Tensor empty_like_device(const at::Tensor& like, at::IntArrayRef sizes, at::ScalarType type) {
+    if (like.is_cuda() && like.device().index() == c10::cuda::current_device())
+        return at::detail::empty_generic(sizes, c10::GetAllocator(c10::kCUDA), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
+    return at::empty(sizes, at::TensorOptions().dtype(type).device(like.device()));
+}
 // A plain matrix on the device of a tensor; rows None: a vector.
 PyObject* new_plain(PyObject*, PyObject* const* args, Py_ssize_t n) {           // like, rows, cols, bf16
     try {
@@ -456,8 +493,9 @@ PyObject* new_plain(PyObject*, PyObject* const* args, Py_ssize_t n) {           
             if (rows == -1 && PyErr_Occurred()) throw Failed();
         }
         const int64_t cols = static_cast<int64_t>(a.u64());
-        const auto options = at::TensorOptions().dtype(a.u32() ? at::kBFloat16 : at::kFloat).device(like.device());
-        return THPVariable_Wrap(r == Py_None ? at::empty({cols}, options) : at::empty({rows, cols}, options));
+        const at::ScalarType type = a.u32() ? at::kBFloat16 : at::kFloat;
+        const int64_t sizes[2] = {rows, cols};
+        return THPVariable_Wrap(empty_like_device(like, r == Py_None ? at::IntArrayRef(&cols, 1) : at::IntArrayRef(sizes, 2), type));
     } catch (const Failed&) {
         return nullptr;
     } catch (const std::exception& e) {
@@ -465,29 +503,30 @@ PyObject* new_plain(PyObject*, PyObject* const* args, Py_ssize_t n) {           
         return nullptr;
     }
 }
-// Memory for a matrix: (codes, scales).  Rows of codes that are longer than 128 bytes start on such a boundary: the products load 128 bytes of a row at a time.
-PyObject* new_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {              // rows, cols, layout, device index
+// Memory for a matrix, on the device of a tensor.
+PyObject* new_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {              // like, rows, cols, layout
     try {
         Args a(args, n);
+        const at::Tensor& like = a.tensor();
         const uint64_t rows = a.u64(), cols = a.u64(), layout = a.u64();
-        const int64_t device = static_cast<int64_t>(a.u64());
         if (rows >= (1ull << 31) || cols > (1ull << 40)) fail(PyExc_ValueError, "a matrix of this size is not possible");
-        const int64_t width = static_cast<int64_t>((cols + 31) / 32 * 16), high = static_cast<int64_t>(rows);
-        const int64_t stride = width > 128 ? (width + 127) / 128 * 128 : width;
-        const bool tiles = layout == TQ_MX_TILES;
-        const int64_t s_rows = tiles ? (high + 127) / 128 : high, s_width = tiles ? (width / 16 + 3) / 4 * 512 : (width / 16 + 15) / 16 * 16;
-        const auto options = at::TensorOptions().dtype(at::kByte).device(at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device)));
-        at::Tensor codes = at::empty({high, stride}, options), scales = at::empty({s_rows, s_width}, options);
-        if (stride != width) codes = codes.as_strided({high, width}, {stride, 1});
-        PyObject* pair = PyTuple_New(2);
-        if (!pair) return nullptr;
-        PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(std::move(codes)));
-        PyTuple_SET_ITEM(pair, 1, THPVariable_Wrap(std::move(scales)));
-        return pair;
+        const int64_t bytes = static_cast<int64_t>(mx_place(rows, cols, layout == TQ_MX_TILES).bytes);
+        return THPVariable_Wrap(empty_like_device(like, at::IntArrayRef(&bytes, 1), at::kByte));
     } catch (const Failed&) {
         return nullptr;
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+// Where it is: (bytes of a row, row stride, first byte of the scales, their rows, their stride).
+PyObject* mx_layout(PyObject*, PyObject* const* args, Py_ssize_t n) {           // rows, cols, layout
+    try {
+        Args a(args, n);
+        const uint64_t rows = a.u64(), cols = a.u64(), layout = a.u64();
+        const MxPlace p = mx_place(rows, cols, layout == TQ_MX_TILES);
+        return Py_BuildValue("KKKKK", p.width, p.stride, p.scales, p.scale_rows, p.scale_stride);
+    } catch (const Failed&) {
         return nullptr;
     }
 }
@@ -581,6 +620,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(bind), METH_FASTCALL, nullptr},
     {"new_mx", reinterpret_cast<PyCFunction>(new_mx), METH_FASTCALL, nullptr},
+    {"mx_layout", reinterpret_cast<PyCFunction>(mx_layout), METH_FASTCALL, nullptr},
     {"new_plain", reinterpret_cast<PyCFunction>(new_plain), METH_FASTCALL, nullptr},
     TQ_ENTRY(stats), TQ_ENTRY(stats_hinted), TQ_ENTRY(stats_static), TQ_ENTRY(params_batch), TQ_ENTRY(params_device), TQ_ENTRY(compress),
     TQ_ENTRY(compress_device_params), TQ_ENTRY(decompress_aggregate), TQ_ENTRY(decompress_aggregate_rows), TQ_ENTRY(decompress_aggregate_apply),
@@ -593,7 +633,7 @@ PyModuleDef module{PyModuleDef_HEAD_INIT, "_tq_python", "Argument marshalling fo
 
 PyMODINIT_FUNC PyInit__tq_python() {
     N = MxNames{PyUnicode_InternFromString("codes"), PyUnicode_InternFromString("scales"), PyUnicode_InternFromString("rows"), PyUnicode_InternFromString("cols"),
-                PyUnicode_InternFromString("layout")};
-    if (!N.codes || !N.scales || !N.rows || !N.cols || !N.layout) return nullptr;
+                PyUnicode_InternFromString("layout"), PyUnicode_InternFromString("memory")};
+    if (!N.codes || !N.scales || !N.rows || !N.cols || !N.layout || !N.memory) return nullptr;
     return PyModule_Create(&module);
 }
