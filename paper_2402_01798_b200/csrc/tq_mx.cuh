@@ -176,7 +176,11 @@ template <bool GELU>
 __device__ __forceinline__ float gate_sigmoid(float x) {
     float z = x;
     if constexpr (GELU) z = kGeluC * x * fmaf(kGeluB * x, x, 1.0f);
-    return __fdividef(1.0f, 1.0f + __expf(-z));
+    // 2^(-z log2 e) and 1 / (1 + that), without the steps for subnormal numbers: below 2^-126 the sigmoid is 0 here
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
+    return s;
 }
 template <bool GELU>
 __device__ __forceinline__ float gate_value(float x) { return x * gate_sigmoid<GELU>(x); }
