@@ -87,7 +87,7 @@ struct MxTile {
     float v[kTileRows * kTilePitch + 16];
     uint32_t random[kTileRows * 64 + 8];   // 16 bits an element, inverted, in 16-byte chunks of 8; see random_chunk.  Not there where rounding is to nearest
 };
-constexpr size_t tile_bytes(bool stochastic) { return stochastic ? sizeof(MxTile) : offsetof(MxTile, random); }
+__host__ __device__ constexpr size_t tile_bytes(bool stochastic) { return stochastic ? sizeof(MxTile) : offsetof(MxTile, random); }
 __device__ __forceinline__ int tile_at(int r, int c) { return r * kTilePitch + (r >> 5) * 16 + (c >> 5) * 36 + (c & 31); }
 // Word of the 16-byte chunk with the bits of row r, columns 8g .. 8g + 7.  The exchange of chunks keeps eight threads that write (two rows,
 // four blocks) in different banks.
@@ -443,51 +443,103 @@ struct MxGatedInput {
     uint64_t dh_stride, gu_stride, features;
     uint32_t wide;                 // the boundary that all rows start on: 32 bytes, 16, or 0 for any
 };
-template <bool BF16, bool GELU, bool STOCHASTIC>
-__global__ void __launch_bounds__(kThreads, 2) mx_gated_backward_kernel(MxGatedInput in, MxView dgu, MxView dgu_t, MxView h_t, uint32_t tiles_across, RoundKeys keys) {
+// bf16 rows on 16-byte boundaries come ahead: while a block works on one tile, its 64 x 128 of dh, g and u for the next are copied into shared memory
+// (asynchronously, whole lines by neighbouring threads, chunks of 16 bytes exchanged as in random_chunk).
+constexpr int kInputs = 3;
+struct MxAhead {
+    uint4 v[kInputs][kTileRows * 16];
+};
+__device__ __forceinline__ int ahead_chunk(int r, int g) { return r * 16 + (g ^ ((g >> 3) | ((r & 1) << 1))); }
+__device__ __forceinline__ void copy_ahead(MxAhead& a, const MxGatedInput& in, uint64_t r0, uint64_t c0, int height, int width) {
+#pragma unroll
+    for (int j = 0; j < kInputs; ++j) {
+        const char* const base = static_cast<const char*>(j == 0 ? in.dh : in.gu);
+        const uint64_t stride = j == 0 ? in.dh_stride : in.gu_stride, from = r0 * stride + c0 + (j == 2 ? in.features : 0);
+#pragma unroll
+        for (int i = 0; i < kTileRows * 16 / kThreads; ++i) {
+            const int at = threadIdx.x + i * kThreads, r = at >> 4, g = at & 15;
+            const bool inside = r < height && g * 8 < width;
+            const char* const src = base + (inside ? (from + r * stride + g * 8) * 2 : 0);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(&a.v[j][ahead_chunk(r, g)])), "l"(src), "r"(inside ? 16 : 0) : "memory");
+        }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void take_ahead(const MxAhead& a, int j, const MxItem& it, float (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint4 w = a.v[j][ahead_chunk(it.r, it.b * 4 + i)];
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { v[8 * i + 2 * k] = __uint_as_float(x[k] << 16); v[8 * i + 2 * k + 1] = __uint_as_float(x[k] & 0xFFFF0000u); }
+    }
+}
+
+// A block takes tile after tile.  AHEAD: as above, 102 KB of shared memory, two blocks an SM.
+template <bool BF16, bool AHEAD, bool GELU, bool STOCHASTIC>
+__global__ void __launch_bounds__(kThreads, 2) mx_gated_backward_kernel(MxGatedInput in, MxView dgu, MxView dgu_t, MxView h_t, uint32_t tiles_across, uint32_t tiles, RoundKeys keys) {
     extern __shared__ __align__(16) unsigned char raw[];
     MxTile& t = *reinterpret_cast<MxTile*>(raw);
+    MxAhead& ahead = *reinterpret_cast<MxAhead*>(raw + tile_bytes(STOCHASTIC));
     pdl_wait();
-    const uint64_t r0 = static_cast<uint64_t>(blockIdx.x / tiles_across) * kTileRows, c0 = static_cast<uint64_t>(blockIdx.x % tiles_across) * kTileCols;
-    const int height = within(dgu.rows, r0, kTileRows), width = within(in.features, c0, kTileCols);
-    const bool last = c0 + kTileCols >= in.features;
     const MxItem it = row_item();
-    const int count = it.r < height ? width - it.b * 32 : 0;
-    const uint64_t row = r0 + it.r, col = c0 + it.b * 32;
-    float dh[32], g[32], u[32];                // become dh, the value and the slope of the activation, and what is made of them
-    load_row_block<BF16>(in.dh, row * in.dh_stride + col, in.wide, count, dh);
-    load_row_block<BF16>(in.gu, row * in.gu_stride + col, in.wide, count, g);
-    load_row_block<BF16>(in.gu, row * in.gu_stride + in.features + col, in.wide, count, u);
-    float x[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        float a, slope;
-        gate_value_slope<GELU>(g[i], a, slope);
-        x[i] = dh[i] * u[i] * slope;           // dg
-        dh[i] = dh[i] * a;                     // du
-        u[i] = a * u[i];                       // h
-    }
+    const auto row_of = [&](uint32_t tile) { return static_cast<uint64_t>(tile / tiles_across) * kTileRows; };
+    const auto col_of = [&](uint32_t tile) { return static_cast<uint64_t>(tile % tiles_across) * kTileCols; };
+    const auto ask = [&](uint32_t tile) {
+        copy_ahead(ahead, in, row_of(tile), col_of(tile), within(dgu.rows, row_of(tile), kTileRows), within(in.features, col_of(tile), kTileCols));
+    };
+    if constexpr (AHEAD) ask(blockIdx.x);
 #pragma unroll 1
-    for (int part = 0; part < 2; ++part) {
-        const uint64_t at = part ? in.features + c0 : c0;
-        put_row(t, it, x);
-        encode_row<STOCHASTIC, true>(t, it, x, dgu, r0, at, height, width, false, keys, 0);
-        __syncthreads();
-        encode_col<STOCHASTIC>(t, dgu_t, at, r0, height, width, false);
-        __syncthreads();
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint64_t r0 = row_of(tile), c0 = col_of(tile);
+        const int height = within(dgu.rows, r0, kTileRows), width = within(in.features, c0, kTileCols);
+        const bool last = c0 + kTileCols >= in.features;
+        float dh[32], g[32], u[32];                // become du, dg and h
+        if constexpr (AHEAD) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncthreads();                       // also: the tile's last reader is through
+            take_ahead(ahead, 0, it, dh); take_ahead(ahead, 1, it, g); take_ahead(ahead, 2, it, u);
+        } else {
+            const int count = it.r < height ? width - it.b * 32 : 0;
+            const uint64_t row = r0 + it.r, col = c0 + it.b * 32;
+            load_row_block<BF16>(in.dh, row * in.dh_stride + col, in.wide, count, dh);
+            load_row_block<BF16>(in.gu, row * in.gu_stride + col, in.wide, count, g);
+            load_row_block<BF16>(in.gu, row * in.gu_stride + in.features + col, in.wide, count, u);
+            __syncthreads();
+        }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) { x[i] = dh[i]; }
+        for (int i = 0; i < 32; ++i) {
+            float a, slope;
+            gate_value_slope<GELU>(g[i], a, slope);
+            g[i] = dh[i] * u[i] * slope;
+            dh[i] = dh[i] * a;
+            u[i] = a * u[i];
+        }
+        // h first: it takes no random numbers, whose registers beside those of all three would not do
+        put_row(t, it, u);
+        __syncthreads();
+        if constexpr (AHEAD)
+            if (tile + gridDim.x < tiles) ask(tile + gridDim.x);
+        encode_col<false>(t, h_t, c0, r0, height, width, last);
+#pragma unroll 1
+        for (int part = 0; part < 2; ++part) {
+            const uint64_t at = part ? in.features + c0 : c0;
+            __syncthreads();
+            put_row(t, it, g);
+            encode_row<STOCHASTIC, true>(t, it, g, dgu, r0, at, height, width, false, keys, 0);
+            __syncthreads();
+            encode_col<STOCHASTIC>(t, dgu_t, at, r0, height, width, false);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) g[i] = dh[i];
+        }
+        // [dg | du] ends anywhere in its last scale tiles, since du starts behind dg: fill them up from there
+        if (last && dgu.tiles)
+            for (uint64_t block = mx_blocks(dgu.cols) + threadIdx.x / kTileRows; block < (mx_blocks(dgu.cols) + 3) / 4 * 4; block += kThreads / kTileRows)
+                dgu.scales[mx_scale_at(dgu, r0 + threadIdx.x % kTileRows, block)] = 0;
+        if (last && dgu_t.tiles)
+            for (uint64_t q = dgu_t.rows + threadIdx.x / 2; q < (dgu_t.rows + 127) / 128 * 128; q += kThreads / 2)
+                dgu_t.scales[mx_scale_at(dgu_t, q, r0 / 32 + threadIdx.x % 2)] = 0;
     }
-    // [dg | du] ends anywhere in its last scale tiles, since du starts behind dg: fill them up from there
-    if (last && dgu.tiles)
-        for (uint64_t block = mx_blocks(dgu.cols) + threadIdx.x / kTileRows; block < (mx_blocks(dgu.cols) + 3) / 4 * 4; block += kThreads / kTileRows)
-            dgu.scales[mx_scale_at(dgu, r0 + threadIdx.x % kTileRows, block)] = 0;
-    if (last && dgu_t.tiles)
-        for (uint64_t q = dgu_t.rows + threadIdx.x / 2; q < (dgu_t.rows + 127) / 128 * 128; q += kThreads / 2)
-            dgu_t.scales[mx_scale_at(dgu_t, q, r0 / 32 + threadIdx.x % 2)] = 0;
-    put_row(t, it, u);
-    __syncthreads();
-    encode_col<false>(t, h_t, c0, r0, height, width, last);
 }
 
 uint32_t boundary(uint64_t at) { return at % 32 == 0 ? 32 : at % 16 == 0 ? 16 : 0; }
@@ -525,8 +577,15 @@ cudaError_t launch_gated_backward_as(const MxGatedBackwardCall& c) {
     const uint64_t size = BF16 ? 2 : 4;
     const MxGatedInput in{c.dh, c.gu, c.dh_stride, c.gu_stride, features,
                           boundary(reinterpret_cast<uintptr_t>(c.dh) | reinterpret_cast<uintptr_t>(c.gu) | (c.dgu->rows > 1 ? (c.dh_stride | c.gu_stride) * size : 0))};
-    return launch_tiled<mx_gated_backward_kernel<BF16, GELU, STOCHASTIC>>(dim3(static_cast<unsigned>(across * down)), tile_bytes(STOCHASTIC), c.stream, in, mx_view(*c.dgu), mx_view(*c.dgu_t), mx_view(*c.h_t),
-                         static_cast<uint32_t>(across), round_keys(c.seed));
+    const uint64_t tiles = across * down, room = 2 * static_cast<uint64_t>(sm_count());
+    const dim3 grid(static_cast<unsigned>(tiles < room ? tiles : room));
+    if constexpr (BF16)
+        if (in.wide)
+            return launch_tiled<mx_gated_backward_kernel<true, true, GELU, STOCHASTIC>>(grid, tile_bytes(STOCHASTIC) + sizeof(MxAhead), c.stream, in, mx_view(*c.dgu),
+                                                                                       mx_view(*c.dgu_t), mx_view(*c.h_t), static_cast<uint32_t>(across), static_cast<uint32_t>(tiles),
+                                                                                       round_keys(c.seed));
+    return launch_tiled<mx_gated_backward_kernel<BF16, false, GELU, STOCHASTIC>>(grid, tile_bytes(STOCHASTIC), c.stream, in, mx_view(*c.dgu), mx_view(*c.dgu_t), mx_view(*c.h_t),
+                         static_cast<uint32_t>(across), static_cast<uint32_t>(tiles), round_keys(c.seed));
 }
 template <bool BF16, bool GELU>
 cudaError_t launch_gated_backward_as(const MxGatedBackwardCall& c) {
