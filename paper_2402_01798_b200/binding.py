@@ -161,7 +161,7 @@ def _load_native(L: C.CDLL):
     except ImportError as e:
         raise RuntimeError("the compiled marshalling module is missing or does not load: build it with "
                            "`python -m paper_2402_01798_b200.build`") from e
-    _tq_python.bind([C.cast(getattr(L, name), C.c_void_p).value for name in _NATIVE])
+    _tq_python.bind([C.cast(getattr(L, name), C.c_void_p).value for name in _NATIVE], MxMatrix)
     return _tq_python
 
 
@@ -448,11 +448,6 @@ class MxMatrix:
             self._views()
         return self._scales
 
-    @property
-    def like(self) -> torch.Tensor:
-        """A tensor on the matrix's device."""
-        return self._codes if self.memory is None else self.memory
-
 
 def tq_mx_code_stride(cols: int) -> int:
     return int(lib().tq_mx_code_stride(cols))
@@ -464,90 +459,63 @@ def tq_mx_scale_stride(cols: int, layout: int = MX_TILES) -> int:
 
 def new_mx(rows: int, cols: int, layout: int = MX_TILES, device="cuda") -> MxMatrix:
     """Memory for a matrix, uninitialised; the calls that write one write all of it, the filling of its last scale tiles included."""
-    return _new_mx(torch.empty(0, dtype=torch.uint8, device=device), rows, cols, layout)
+    return _calls().new_mx(torch.empty(0, dtype=torch.uint8, device=device), rows, cols, layout)
 
 
-def _new_mx(like: torch.Tensor, rows: int, cols: int, layout: int) -> MxMatrix:
-    return MxMatrix(None, None, rows, cols, layout, _calls().new_mx(like, rows, cols, layout))
+def _made(result, where: str):
+    """What a call of the compiled module made, or an error for the status it came back with."""
+    if result.__class__ is int:
+        _check(result, where)
+    return result
 
 
-def _new_plain(like: torch.Tensor, rows: Optional[int], cols: int, dtype: torch.dtype) -> torch.Tensor:
-    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+def _is_bf16(dtype: torch.dtype) -> bool:
+    if dtype is torch.bfloat16:
+        return True
+    if dtype is not torch.float32:
         raise TypeError("float32 or bfloat16 is needed")
-    return _calls().new_plain(like, rows, cols, dtype is torch.bfloat16)
-
-
-def _seed(seed: int) -> int:
-    return seed & 0xFFFFFFFFFFFFFFFF
+    return False
 
 
 def tq_mx_quantize(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int = 0, first_row: int = 0, cols: Optional[int] = None,
                    layout: int = MX_TILES, out: Optional[MxMatrix] = None, stream=None) -> MxMatrix:
     """Enqueue the quantisation of ``x`` ([rows, cols] or [cols], fp32 or bf16) along its rows; the first ``cols`` columns when given."""
-    if out is None:
-        out = _new_mx(x, _rows(x), x.size(-1) if cols is None else cols, layout)
-    _check(_calls().mx_quantize(x, rounding, _seed(seed), first_row, out, stream), "tq_mx_quantize")
-    return out
+    return _made(_calls().mx_quantize(x, rounding, seed, first_row, cols, layout, out, stream), "tq_mx_quantize")
 
 
 def tq_mx_quantize_both(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int = 0, first_row: int = 0, out: Optional[MxMatrix] = None,
                         out_t: Optional[MxMatrix] = None, stream=None) -> Tuple[MxMatrix, MxMatrix]:
     """``x`` along its rows, and its transposed copy, whose blocks run along x's columns."""
-    if out is None:
-        out = _new_mx(x, _rows(x), x.size(-1), MX_TILES)
-    if out_t is None:
-        out_t = _new_mx(x, out.cols, out.rows, MX_TILES)
-    _check(_calls().mx_quantize_both(x, rounding, _seed(seed), first_row, out, out_t, stream), "tq_mx_quantize_both")
-    return out, out_t
+    return _made(_calls().mx_quantize_both(x, rounding, seed, first_row, out, out_t, stream), "tq_mx_quantize_both")
 
 
 def tq_mx_dequantize(m: MxMatrix, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The values of ``m`` as a [rows, cols] tensor."""
-    if out is None:
-        out = _new_plain(m.like, m.rows, m.cols, dtype)
-    _check(_calls().mx_dequantize(m, out, stream), "tq_mx_dequantize")
-    return out
+    return _made(_calls().mx_dequantize(m, _is_bf16(dtype), out, stream), "tq_mx_dequantize")
 
 
 def tq_mx_decompress_aggregate(m: MxMatrix, weights: Optional[Sequence[float]] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue the mean (or weighted sum) of the rows of ``m`` (layout MX_ROWS); returns the [cols] fp32 update."""
-    if out is None:
-        out = _new_plain(m.like, None, m.cols, torch.float32)
-    _check(_calls().mx_decompress_aggregate(m, weights, out, stream), "tq_mx_decompress_aggregate")
-    return out
+    return _made(_calls().mx_decompress_aggregate(m, weights, out, stream), "tq_mx_decompress_aggregate")
 
 
 def tq_mx_product(a: MxMatrix, b: MxMatrix, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue a b^T; returns [a.rows, b.rows]."""
-    if out is None:
-        out = _new_plain(a.like, a.rows, b.rows, dtype)
-    _check(_calls().mx_product(a, b, out, stream), "tq_mx_product")
-    return out
+    return _made(_calls().mx_product(a, b, _is_bf16(dtype), out, stream), "tq_mx_product")
 
 
 def tq_mx_gated(x: MxMatrix, w_gate: MxMatrix, w_up: MxMatrix, activation: int = MX_SILU, projections: Optional[torch.Tensor] = None,
                 out: Optional[MxMatrix] = None, stream=None) -> MxMatrix:
     """Enqueue act(x w_gate^T) * (x w_up^T), quantised along its rows.  ``projections``: a [tokens, 2 features] tensor that receives both
     projections, for tq_mx_gated_backward."""
-    if out is None:
-        out = _new_mx(x.like, x.rows, w_gate.rows, MX_TILES)
-    _check(_calls().mx_gated(x, w_gate, w_up, activation, out, projections, stream), "tq_mx_gated")
-    return out
+    return _made(_calls().mx_gated(x, w_gate, w_up, activation, projections, out, stream), "tq_mx_gated")
 
 
 def tq_mx_gated_backward(dh: torch.Tensor, projections: torch.Tensor, activation: int = MX_SILU, rounding: int = MX_STOCHASTIC, seed: int = 0,
                          dgu: Optional[MxMatrix] = None, dgu_t: Optional[MxMatrix] = None, h_t: Optional[MxMatrix] = None,
                          stream=None) -> Tuple[MxMatrix, MxMatrix, MxMatrix]:
     """Enqueue the backward pass of tq_mx_gated up to the products; returns ([dg | du], its transposed copy, the transposed h)."""
-    tokens, features = _rows(dh), dh.shape[-1]
-    if dgu is None:
-        dgu = _new_mx(dh, tokens, 2 * features, MX_TILES)
-    if dgu_t is None:
-        dgu_t = _new_mx(dh, 2 * features, tokens, MX_TILES)
-    if h_t is None:
-        h_t = _new_mx(dh, features, tokens, MX_TILES)
-    _check(_calls().mx_gated_backward(dh, projections, activation, rounding, _seed(seed), dgu, dgu_t, h_t, stream), "tq_mx_gated_backward")
-    return dgu, dgu_t, h_t
+    return _made(_calls().mx_gated_backward(dh, projections, activation, rounding, seed, dgu, dgu_t, h_t, stream), "tq_mx_gated_backward")
 
 
 def tq_kernel_launches() -> int:

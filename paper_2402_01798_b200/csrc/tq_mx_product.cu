@@ -491,9 +491,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
                 tma_load(at, &map_b0, c * (kBK / 2), n0, full(s));
                 if constexpr (GATED != 0) tma_load(at + S::kCodesB / 2, &map_b1, c * (kBK / 2), n0, full(s));
                 tma_load(at + at_a, &map_a, c * (kBK / 2), tm * 128, full(s));
-                bulk_load(scales, p.a_scales + tm * p.a_band + c * 1024, bytes, full(s));
-                bulk_load(scales + 1024, p.b0_scales + (n0 / 128) * p.b0_band + c * 1024, bytes, full(s));
-                if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024, bytes, full(s));
+                bulk_load(scales, p.a_scales + tm * p.a_band + c * 1024ull, bytes, full(s));
+                bulk_load(scales + 1024, p.b0_scales + (n0 / 128) * p.b0_band + c * 1024ull, bytes, full(s));
+                if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024ull, bytes, full(s));
             }
             __syncwarp();
             if (++s == stages) { s = 0; ++round; }

@@ -11,6 +11,7 @@
 
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -383,7 +384,7 @@ tq_status decompress_aggregate_segments(Args& a) {           // packed, segments
 
 // ---- microscaled 4-bit floating point: an MxMatrix (binding.py) is six attributes ---------------------------------
 struct MxNames {
-    PyObject *codes, *scales, *rows, *cols, *layout, *memory;
+    PyObject *codes, *scales, *rows, *cols, *layout, *memory, *own_codes, *own_scales;
 } N;
 // A matrix in one piece of memory: codes, and on the next 128-byte boundary scales.  Rows of codes that are longer than 128 bytes start on such a
 // boundary: the products load 128 bytes of a row at a time.
@@ -428,8 +429,7 @@ uint8_t* bytes_of(PyObject* o, PyObject* name, const char* what, uint64_t rows, 
     *stride = t.size(0) > 1 ? static_cast<uint64_t>(t.stride(0)) : static_cast<uint64_t>(t.size(1)) / 16 * 16;
     return static_cast<uint8_t*>(t.data_ptr());
 }
-tq_mx_t mx(Args& a) {
-    PyObject* o = a.next();
+tq_mx_t mx(PyObject* o) {
     tq_mx_t m{};
     m.rows = attribute(o, N.rows); m.cols = attribute(o, N.cols);
     m.layout = static_cast<uint32_t>(attribute(o, N.layout));
@@ -481,112 +481,179 @@ at::Tensor empty_like_device(const at::Tensor& like, at::IntArrayRef sizes, at::
         return at::detail::empty_generic(sizes, c10::GetAllocator(c10::kCUDA), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
     return at::empty(sizes, at::TensorOptions().dtype(type).device(like.device()));
 }
-// A plain matrix on the device of a tensor; rows None: a vector.
-PyObject* new_plain(PyObject*, PyObject* const* args, Py_ssize_t n) {           // like, rows, cols, bf16
-    try {
-        Args a(args, n);
-        const at::Tensor& like = a.tensor();
-        PyObject* r = a.next();
-        int64_t rows = 0;
-        if (r != Py_None) {
-            rows = PyLong_AsLongLong(r);
-            if (rows == -1 && PyErr_Occurred()) throw Failed();
-        }
-        const int64_t cols = static_cast<int64_t>(a.u64());
-        const at::ScalarType type = a.u32() ? at::kBFloat16 : at::kFloat;
-        const int64_t sizes[2] = {rows, cols};
-        return THPVariable_Wrap(empty_like_device(like, r == Py_None ? at::IntArrayRef(&cols, 1) : at::IntArrayRef(sizes, 2), type));
-    } catch (const Failed&) {
-        return nullptr;
-    } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
-    }
+// A Python object that this call owns until it hands it over.
+class Owned {
+public:
+    explicit Owned(PyObject* o = nullptr) : o_(o) {}
+    Owned(Owned&& other) : o_(other.o_) { other.o_ = nullptr; }
+    ~Owned() { Py_XDECREF(o_); }
+    Owned(const Owned&) = delete;
+    PyObject* get() const { return o_; }
+    PyObject* release() { PyObject* o = o_; o_ = nullptr; return o; }
+
+private:
+    PyObject* o_;
+};
+PyObject* mx_class = nullptr;                   // binding.MxMatrix
+
+// A matrix in memory of its own, on the device of a tensor.
+Owned new_matrix(const at::Tensor& like, uint64_t rows, uint64_t cols, uint64_t layout) {
+    if (rows >= (1ull << 31) || cols > (1ull << 40)) fail(PyExc_ValueError, "a matrix of this size is not possible");
+    const int64_t bytes = static_cast<int64_t>(mx_place(rows, cols, layout == TQ_MX_TILES).bytes);
+    static PyObject* const nothing = PyTuple_New(0);
+    PyTypeObject* const type = reinterpret_cast<PyTypeObject*>(mx_class);
+    Owned m(type->tp_new(type, nothing, nullptr));
+    if (!m.get()) throw Failed();
+    const auto set = [&](PyObject* name, PyObject* value) {
+        const Owned v(value);
+        if (!value || PyObject_SetAttr(m.get(), name, value) != 0) throw Failed();
+    };
+    set(N.memory, THPVariable_Wrap(empty_like_device(like, at::IntArrayRef(&bytes, 1), at::kByte)));
+    set(N.rows, PyLong_FromUnsignedLongLong(rows));
+    set(N.cols, PyLong_FromUnsignedLongLong(cols));
+    set(N.layout, PyLong_FromUnsignedLongLong(layout));
+    Py_INCREF(Py_None);
+    set(N.own_codes, Py_None);
+    Py_INCREF(Py_None);
+    set(N.own_scales, Py_None);
+    return m;
 }
-// Memory for a matrix, on the device of a tensor.
-PyObject* new_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {              // like, rows, cols, layout
-    try {
-        Args a(args, n);
-        const at::Tensor& like = a.tensor();
-        const uint64_t rows = a.u64(), cols = a.u64(), layout = a.u64();
-        if (rows >= (1ull << 31) || cols > (1ull << 40)) fail(PyExc_ValueError, "a matrix of this size is not possible");
-        const int64_t bytes = static_cast<int64_t>(mx_place(rows, cols, layout == TQ_MX_TILES).bytes);
-        return THPVariable_Wrap(empty_like_device(like, at::IntArrayRef(&bytes, 1), at::kByte));
-    } catch (const Failed&) {
-        return nullptr;
-    } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
-    }
-}
-// Where it is: (bytes of a row, row stride, first byte of the scales, their rows, their stride).
-PyObject* mx_layout(PyObject*, PyObject* const* args, Py_ssize_t n) {           // rows, cols, layout
-    try {
-        Args a(args, n);
-        const uint64_t rows = a.u64(), cols = a.u64(), layout = a.u64();
-        const MxPlace p = mx_place(rows, cols, layout == TQ_MX_TILES);
-        return Py_BuildValue("KKKKK", p.width, p.stride, p.scales, p.scale_rows, p.scale_stride);
-    } catch (const Failed&) {
-        return nullptr;
-    }
-}
-tq_status mx_quantize(Args& a) {                // x, rounding, seed, first_row, out, stream
-    const at::Tensor& x = a.tensor();
-    const uint32_t rounding = a.u32();
-    const uint64_t seed = a.u64();
-    const uint32_t first = a.u32();
-    const tq_mx_t out = mx(a);
-    const Plain p = plain(x, "x", out.rows, out.cols);
-    return call(F.mx_quantize, p.data, p.dtype, p.stride, static_cast<tq_mx_rounding>(rounding), seed, first, &out, a.stream());
-}
-tq_status mx_quantize_both(Args& a) {           // x, rounding, seed, first_row, out, out_t, stream
-    const at::Tensor& x = a.tensor();
-    const uint32_t rounding = a.u32();
-    const uint64_t seed = a.u64();
-    const uint32_t first = a.u32();
-    const tq_mx_t out = mx(a), out_t = mx(a);
-    const Plain p = plain(x, "x", out.rows, out.cols);
-    return call(F.mx_quantize_both, p.data, p.dtype, p.stride, static_cast<tq_mx_rounding>(rounding), seed, first, &out, &out_t, a.stream());
-}
-tq_status mx_dequantize(Args& a) {              // matrix, out, stream
-    const tq_mx_t m = mx(a);
-    const Plain p = plain(a.tensor(), "out", m.rows, m.cols);
-    return call(F.mx_dequantize, &m, p.data, p.dtype, p.stride, a.stream());
-}
-tq_status mx_decompress_aggregate(Args& a) {    // matrix, weights, out, stream
-    const tq_mx_t m = mx(a);
-    const float* w = a.weights(static_cast<uint32_t>(m.rows < TQ_MAX_WORKERS ? m.rows : TQ_MAX_WORKERS));
-    const Plain p = plain(a.tensor(), "out", 1, m.cols);
-    if (p.dtype != TQ_F32) fail(PyExc_TypeError, "out must be float32");
-    return call(F.mx_decompress_aggregate, &m, w, static_cast<float*>(p.data), a.stream());
-}
-tq_status mx_product(Args& a) {                 // a, b, out, stream
-    const tq_mx_t x = mx(a), y = mx(a);
-    const Plain p = plain(a.tensor(), "out", x.rows, y.rows);
-    return call(F.mx_product, &x, &y, p.data, p.dtype, p.stride, a.stream());
-}
-tq_status mx_gated(Args& a) {                   // x, w_gate, w_up, activation, h, projections, stream
-    const tq_mx_t x = mx(a), wg = mx(a), wu = mx(a);
-    const uint32_t act = a.u32();
-    const tq_mx_t h = mx(a);
+// The next argument, or for None a new matrix.
+Owned matrix_or_new(Args& a, const at::Tensor& like, uint64_t rows, uint64_t cols, uint64_t layout) {
     PyObject* o = a.next();
-    Plain p{nullptr, TQ_F32, 0};
+    if (o == Py_None) return new_matrix(like, rows, cols, layout);
+    Py_INCREF(o);
+    return Owned(o);
+}
+// The next argument, or for None a new [rows, cols] tensor; with rows -1 a vector.
+Owned tensor_or_new(Args& a, const at::Tensor& like, int64_t rows, int64_t cols, bool bf16) {
+    PyObject* o = a.next();
     if (o != Py_None) {
         if (!THPVariable_Check(o)) fail(PyExc_TypeError, "a tensor is needed");
-        p = plain(THPVariable_Unpack(o), "projections", x.rows, 2 * wg.rows);
+        Py_INCREF(o);
+        return Owned(o);
     }
-    return call(F.mx_gated, &x, &wg, &wu, static_cast<tq_mx_activation>(act), &h, p.data, p.dtype, p.stride, a.stream());
+    const int64_t sizes[2] = {rows, cols};
+    Owned t(THPVariable_Wrap(empty_like_device(like, rows < 0 ? at::IntArrayRef(&cols, 1) : at::IntArrayRef(sizes, 2), bf16 ? at::kBFloat16 : at::kFloat)));
+    if (!t.get()) throw Failed();
+    return t;
 }
-tq_status mx_gated_backward(Args& a) {          // dh, projections, activation, rounding, seed, dgu, dgu_t, h_t, stream
+// Some tensor of a matrix, for its device.
+const at::Tensor& tensor_of(PyObject* matrix) {
+    PyObject* v = PyObject_GetAttr(matrix, N.memory);
+    if (!v) throw Failed();
+    Py_DECREF(v);                                                  // held by the matrix
+    if (v == Py_None) {
+        v = PyObject_GetAttr(matrix, N.codes);
+        if (!v) throw Failed();
+        Py_DECREF(v);
+    }
+    if (!THPVariable_Check(v)) fail(PyExc_TypeError, "codes and scales must be tensors");
+    return THPVariable_Unpack(v);
+}
+uint64_t high(const at::Tensor& t) { return t.dim() == 2 ? static_cast<uint64_t>(t.size(0)) : 1u; }
+uint64_t wide(const at::Tensor& t) {
+    if (t.dim() < 1) fail(PyExc_ValueError, "a matrix or a vector is needed");
+    return static_cast<uint64_t>(t.size(t.dim() - 1));
+}
+
+// These calls return what they made, or the library's status.
+PyObject* made(tq_status s, Owned& o) { return s == TQ_OK ? o.release() : PyLong_FromLong(s); }
+PyObject* made(tq_status s, std::initializer_list<Owned*> all) {
+    if (s != TQ_OK) return PyLong_FromLong(s);
+    PyObject* t = PyTuple_New(static_cast<Py_ssize_t>(all.size()));
+    if (!t) throw Failed();
+    Py_ssize_t i = 0;
+    for (Owned* o : all) PyTuple_SET_ITEM(t, i++, o->release());
+    return t;
+}
+PyObject* new_mx(Args& a) {                     // like, rows, cols, layout
+    const at::Tensor& like = a.tensor();
+    const uint64_t rows = a.u64(), cols = a.u64(), layout = a.u64();
+    return new_matrix(like, rows, cols, layout).release();
+}
+// Where a matrix in one piece is: (bytes of a row, row stride, first byte of the scales, their rows, their stride).
+PyObject* mx_layout(Args& a) {                  // rows, cols, layout
+    const uint64_t rows = a.u64(), cols = a.u64(), layout = a.u64();
+    const MxPlace p = mx_place(rows, cols, layout == TQ_MX_TILES);
+    return Py_BuildValue("KKKKK", p.width, p.stride, p.scales, p.scale_rows, p.scale_stride);
+}
+PyObject* mx_quantize(Args& a) {                // x, rounding, seed, first_row, cols, layout, out, stream
+    const at::Tensor& x = a.tensor();
+    const uint32_t rounding = a.u32();
+    const uint64_t seed = a.u64();
+    const uint32_t first = a.u32();
+    PyObject* c = a.next();
+    const uint64_t cols = c == Py_None ? wide(x) : PyLong_AsUnsignedLongLong(c), layout = a.u64();
+    if (PyErr_Occurred()) throw Failed();
+    Owned out = matrix_or_new(a, x, high(x), cols, layout);
+    const tq_mx_t m = mx(out.get());
+    const Plain p = plain(x, "x", m.rows, m.cols);
+    return made(call(F.mx_quantize, p.data, p.dtype, p.stride, static_cast<tq_mx_rounding>(rounding), seed, first, &m, a.stream()), out);
+}
+PyObject* mx_quantize_both(Args& a) {           // x, rounding, seed, first_row, out, out_t, stream
+    const at::Tensor& x = a.tensor();
+    const uint32_t rounding = a.u32();
+    const uint64_t seed = a.u64();
+    const uint32_t first = a.u32();
+    Owned out = matrix_or_new(a, x, high(x), wide(x), TQ_MX_TILES);
+    const tq_mx_t m = mx(out.get());
+    Owned out_t = matrix_or_new(a, x, m.cols, m.rows, TQ_MX_TILES);
+    const tq_mx_t m_t = mx(out_t.get());
+    const Plain p = plain(x, "x", m.rows, m.cols);
+    return made(call(F.mx_quantize_both, p.data, p.dtype, p.stride, static_cast<tq_mx_rounding>(rounding), seed, first, &m, &m_t, a.stream()), {&out, &out_t});
+}
+PyObject* mx_dequantize(Args& a) {              // matrix, bf16, out, stream
+    PyObject* o = a.next();
+    const tq_mx_t m = mx(o);
+    const bool bf16 = a.u32() != 0;
+    Owned out = tensor_or_new(a, tensor_of(o), static_cast<int64_t>(m.rows), static_cast<int64_t>(m.cols), bf16);
+    const Plain p = plain(THPVariable_Unpack(out.get()), "out", m.rows, m.cols);
+    return made(call(F.mx_dequantize, &m, p.data, p.dtype, p.stride, a.stream()), out);
+}
+PyObject* mx_decompress_aggregate(Args& a) {    // matrix, weights, out, stream
+    PyObject* o = a.next();
+    const tq_mx_t m = mx(o);
+    const float* w = a.weights(static_cast<uint32_t>(m.rows < TQ_MAX_WORKERS ? m.rows : TQ_MAX_WORKERS));
+    Owned out = tensor_or_new(a, tensor_of(o), -1, static_cast<int64_t>(m.cols), false);
+    const Plain p = plain(THPVariable_Unpack(out.get()), "out", 1, m.cols);
+    if (p.dtype != TQ_F32) fail(PyExc_TypeError, "out must be float32");
+    return made(call(F.mx_decompress_aggregate, &m, w, static_cast<float*>(p.data), a.stream()), out);
+}
+PyObject* mx_product(Args& a) {                 // a, b, bf16, out, stream
+    PyObject* o = a.next();
+    const tq_mx_t x = mx(o), y = mx(a.next());
+    const bool bf16 = a.u32() != 0;
+    Owned out = tensor_or_new(a, tensor_of(o), static_cast<int64_t>(x.rows), static_cast<int64_t>(y.rows), bf16);
+    const Plain p = plain(THPVariable_Unpack(out.get()), "out", x.rows, y.rows);
+    return made(call(F.mx_product, &x, &y, p.data, p.dtype, p.stride, a.stream()), out);
+}
+PyObject* mx_gated(Args& a) {                   // x, w_gate, w_up, activation, projections, out, stream
+    PyObject* o = a.next();
+    const tq_mx_t x = mx(o), wg = mx(a.next()), wu = mx(a.next());
+    const uint32_t act = a.u32();
+    PyObject* kept = a.next();
+    Plain p{nullptr, TQ_F32, 0};
+    if (kept != Py_None) {
+        if (!THPVariable_Check(kept)) fail(PyExc_TypeError, "a tensor is needed");
+        p = plain(THPVariable_Unpack(kept), "projections", x.rows, 2 * wg.rows);
+    }
+    Owned out = matrix_or_new(a, tensor_of(o), x.rows, wg.rows, TQ_MX_TILES);
+    const tq_mx_t h = mx(out.get());
+    return made(call(F.mx_gated, &x, &wg, &wu, static_cast<tq_mx_activation>(act), &h, p.data, p.dtype, p.stride, a.stream()), out);
+}
+PyObject* mx_gated_backward(Args& a) {          // dh, projections, activation, rounding, seed, dgu, dgu_t, h_t, stream
     const at::Tensor& dh = a.tensor();
     const at::Tensor& gu = a.tensor();
     const uint32_t act = a.u32(), rounding = a.u32();
-    const uint64_t seed = a.u64();
-    const tq_mx_t dgu = mx(a), dgu_t = mx(a), h_t = mx(a);
-    const Plain p = plain(dh, "dh", dgu.rows, h_t.rows), q = plain(gu, "projections", dgu.rows, dgu.cols);
+    const uint64_t seed = a.u64(), tokens = high(dh), features = wide(dh);
+    Owned dgu = matrix_or_new(a, dh, tokens, 2 * features, TQ_MX_TILES), dgu_t = matrix_or_new(a, dh, 2 * features, tokens, TQ_MX_TILES);
+    Owned h_t = matrix_or_new(a, dh, features, tokens, TQ_MX_TILES);
+    const tq_mx_t m = mx(dgu.get()), m_t = mx(dgu_t.get()), h = mx(h_t.get());
+    const Plain p = plain(dh, "dh", m.rows, h.rows), q = plain(gu, "projections", m.rows, m.cols);
     if (p.dtype != q.dtype) fail(PyExc_TypeError, "dh and projections must be of one type");
-    return call(F.mx_gated_backward, p.data, p.stride, q.data, q.stride, p.dtype, static_cast<tq_mx_activation>(act), static_cast<tq_mx_rounding>(rounding), seed, &dgu, &dgu_t,
-                &h_t, a.stream());
+    return made(call(F.mx_gated_backward, p.data, p.stride, q.data, q.stride, p.dtype, static_cast<tq_mx_activation>(act), static_cast<tq_mx_rounding>(rounding), seed, &m, &m_t,
+                     &h, a.stream()), {&dgu, &dgu_t, &h_t});
 }
 
 template <tq_status (*CALL)(Args&)>
@@ -602,10 +669,23 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
 }
 
-// bind([addresses in the order of Functions])
+template <PyObject* (*CALL)(Args&)>
+PyObject* maker(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    try {
+        Args a(args, n);
+        return CALL(a);
+    } catch (const Failed&) {
+        return nullptr;
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// bind([addresses in the order of Functions], MxMatrix)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     constexpr Py_ssize_t count = sizeof(Functions) / sizeof(void*);
-    if (n != 1 || !PyList_Check(args[0]) || PyList_GET_SIZE(args[0]) != count) {
+    if (n < 1 || n > 2 || !PyList_Check(args[0]) || PyList_GET_SIZE(args[0]) != count || (n == 2 && !PyType_Check(args[1]))) {
         PyErr_SetString(PyExc_TypeError, "a list of function addresses is needed");
         return nullptr;
     }
@@ -613,27 +693,31 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     for (Py_ssize_t i = 0; i < count; ++i) p[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(args[0], i));
     if (PyErr_Occurred()) return nullptr;
     memcpy(&F, p, sizeof(F));
+    if (n == 2) {
+        Py_INCREF(args[1]);
+        Py_XDECREF(mx_class);
+        mx_class = args[1];
+    }
     Py_RETURN_NONE;
 }
 
 #define TQ_ENTRY(name) {#name, reinterpret_cast<PyCFunction>(entry<name>), METH_FASTCALL, nullptr}
+#define TQ_MAKER(name) {#name, reinterpret_cast<PyCFunction>(maker<name>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(bind), METH_FASTCALL, nullptr},
-    {"new_mx", reinterpret_cast<PyCFunction>(new_mx), METH_FASTCALL, nullptr},
-    {"mx_layout", reinterpret_cast<PyCFunction>(mx_layout), METH_FASTCALL, nullptr},
-    {"new_plain", reinterpret_cast<PyCFunction>(new_plain), METH_FASTCALL, nullptr},
     TQ_ENTRY(stats), TQ_ENTRY(stats_hinted), TQ_ENTRY(stats_static), TQ_ENTRY(params_batch), TQ_ENTRY(params_device), TQ_ENTRY(compress),
     TQ_ENTRY(compress_device_params), TQ_ENTRY(decompress_aggregate), TQ_ENTRY(decompress_aggregate_rows), TQ_ENTRY(decompress_aggregate_apply),
     TQ_ENTRY(decompress_aggregate_device_params), TQ_ENTRY(stats_segments), TQ_ENTRY(stats_hinted_segments), TQ_ENTRY(compress_segments),
-    TQ_ENTRY(decompress_aggregate_segments), TQ_ENTRY(mx_quantize), TQ_ENTRY(mx_quantize_both), TQ_ENTRY(mx_dequantize), TQ_ENTRY(mx_decompress_aggregate),
-    TQ_ENTRY(mx_product), TQ_ENTRY(mx_gated), TQ_ENTRY(mx_gated_backward), {nullptr, nullptr, 0, nullptr}};
+    TQ_ENTRY(decompress_aggregate_segments), TQ_MAKER(new_mx), TQ_MAKER(mx_layout), TQ_MAKER(mx_quantize), TQ_MAKER(mx_quantize_both), TQ_MAKER(mx_dequantize),
+    TQ_MAKER(mx_decompress_aggregate), TQ_MAKER(mx_product), TQ_MAKER(mx_gated), TQ_MAKER(mx_gated_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module{PyModuleDef_HEAD_INIT, "_tq_python", "Argument marshalling for libtq.so.", -1, methods};
 
 }  // namespace
 
 PyMODINIT_FUNC PyInit__tq_python() {
     N = MxNames{PyUnicode_InternFromString("codes"), PyUnicode_InternFromString("scales"), PyUnicode_InternFromString("rows"), PyUnicode_InternFromString("cols"),
-                PyUnicode_InternFromString("layout"), PyUnicode_InternFromString("memory")};
-    if (!N.codes || !N.scales || !N.rows || !N.cols || !N.layout || !N.memory) return nullptr;
+                PyUnicode_InternFromString("layout"), PyUnicode_InternFromString("memory"),
+                PyUnicode_InternFromString("_codes"), PyUnicode_InternFromString("_scales")};
+    if (!N.codes || !N.scales || !N.rows || !N.cols || !N.layout || !N.memory || !N.own_codes || !N.own_scales) return nullptr;
     return PyModule_Create(&module);
 }
