@@ -712,6 +712,7 @@ cudaError_t codes_map(CUtensorMap* map, const tq_mx_t& m, uint32_t rows) {
 }
 
 // Memory of a split block: its stages, or what it receives.
+constexpr uint32_t kMostSplitSmem = 216 * 1024;                  // beside 10 KB of fixed arrays
 struct SplitMemory {
     uint32_t stages, stage_bytes;
     size_t bytes;
@@ -724,6 +725,7 @@ SplitMemory split_memory(uint32_t rows, uint32_t a_rows, uint64_t chunks, uint32
     if (m.stages > most) m.stages = static_cast<uint32_t>(most);
     const uint32_t sums = split > 1 ? rows * 128 * 4 * (GATED ? 2 : 1) : 0;
     const uint32_t last = S::kCodesA > m.stage_bytes - S::kCodesB ? S::kCodesA : m.stage_bytes - S::kCodesB;      // 128 rows of A from the last box on
+    while ((m.stages - 1) * m.stage_bytes + S::kCodesB + last + 1024 > kMostSplitSmem) --m.stages;
     const uint32_t staged = (m.stages - 1) * m.stage_bytes + S::kCodesB + last;
     // No more blocks on an SM than its tensor memory serves at once, two plain ones, or one gated one and nothing beside it: a block that waits for
     // columns keeps its cluster waiting, and two clusters that hold each other's columns would wait for ever.
@@ -750,7 +752,8 @@ ProductPlan plan_product(uint32_t m, uint32_t n, uint32_t k, uint32_t a_rows) {
     const uint64_t narrow = (static_cast<uint64_t>(m) + 127) / 128 * ((static_cast<uint64_t>(n) + 127) / 128);
     const uint32_t rows = m < 128 ? m : 128;
     for (uint32_t split = 1; split <= (GATED ? 4u : 8u) && split <= chunks; split *= 2) {
-        const bool two = !GATED && split_memory<GATED>(rows, a_rows, chunks, split).bytes <= 100 * 1024;      // beside 10 KB of fixed arrays
+        // two blocks of few rows run side by side on an SM; two with all rows take as long as one after the other (4096 x 1024 x 250: 7.0 us, a pair 5.9)
+        const bool two = !GATED && rows <= 32 && split_memory<GATED>(rows, a_rows, chunks, split).bytes <= 100 * 1024;      // beside 10 KB of fixed arrays
         const uint64_t room = (split == 8 ? sms * 7 / 8 : sms) * (two ? 2 : 1), blocks = narrow * split;
         const uint64_t waves = (blocks + room - 1) / room, stage = (GATED ? 340 : 285) + rows / 5 + 70 * (blocks < sms ? blocks : sms) / sms;
         const uint64_t sums = split == 1 ? 500 : 800 + 100 * split + 4 * rows * split;
@@ -791,7 +794,7 @@ cudaError_t launch_split_as(const CUtensorMap& map_a, const CUtensorMap& map_b0,
     using S = SplitShape<GATED>;
     SplitMemory mem = split_memory<GATED>(p.m < 128 ? p.m : 128, p.a_rows, (static_cast<uint64_t>(p.k) + kBK - 1) / kBK, SPLIT);
     void* args[] = {const_cast<CUtensorMap*>(&map_a), const_cast<CUtensorMap*>(&map_b0), const_cast<CUtensorMap*>(&map_b1), const_cast<ProductArgs*>(&p), &mem.stages, &mem.stage_bytes};
-    return launch_clustered<mx_split_kernel<GATED, SPLIT>>(p.tiles_m * p.tiles_n * SPLIT, SPLIT, kSplitThreads, mem.bytes, S::kMostStageSmem + 2048, stream, args);
+    return launch_clustered<mx_split_kernel<GATED, SPLIT>>(p.tiles_m * p.tiles_n * SPLIT, SPLIT, kSplitThreads, mem.bytes, kMostSplitSmem, stream, args);
 }
 
 template <int GATED>

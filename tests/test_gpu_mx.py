@@ -216,6 +216,24 @@ def test_product(tq, m, n, k, dtype):
     assert np.array_equal(tq.tq_mx_product(a, b, dtype).cpu().double().numpy(), got[:m, :n])
 
 
+@pytest.mark.parametrize("m", [1, 8, 9, 24, 40, 47, 56, 64, 72, 96, 120, 127])
+def test_few_rows_with_long_sums(tq, m):
+    """Every number of rows that is loaded at a time, with more stages of k than fit the chip."""
+    rng = np.random.default_rng(m)
+    for n, k in ((520, 8192), (16_500, 2560)):
+        a, b = random_mx(tq, rng, m, k, 1), random_mx(tq, rng, n, k, 1)
+        va, vb = values(a), values(b)
+        want, got = va @ vb.T, tq.tq_mx_product(a, b, torch.float32).cpu().double().numpy()
+        bound = sum_bound(va, vb, k)
+        assert (np.abs(got - want) <= bound + 2.0 ** -24 * (np.abs(want) + bound)).all()
+    x, wg, wu = random_mx(tq, rng, m, 4096, 1), random_mx(tq, rng, 256, 4096, 1), random_mx(tq, rng, 256, 4096, 1)
+    gu = torch.empty(m, 512, device="cuda")
+    tq.tq_mx_gated(x, wg, wu, projections=gu)
+    for half, w in ((gu[:, :256], wg), (gu[:, 256:], wu)):
+        want, bound = values(x) @ values(w).T, sum_bound(values(x), values(w), 4096)
+        assert (np.abs(half.cpu().double().numpy() - want) <= bound + 2.0 ** -24 * (np.abs(want) + bound)).all()
+
+
 def test_product_scales_reach_the_ends(tq):
     """Every scale byte, and NaN blocks: a row of one operand that holds one is NaN, the others are untouched."""
     rng = np.random.default_rng(4)
