@@ -10,6 +10,9 @@
  *
  * The N clients ("workers") are N gradient slices resident on one GPU.
  *
+ * Beside that path: microscaled 4-bit floating point (tq_mx_*), as a second wire format and as operands of the products of a
+ * training step or of serving.
+ *
  * Conventions
  *   - "dev" pointers are CUDA device pointers owned by the caller; "host" pointers are ordinary
  *     host memory.  The library allocates no device memory and frees nothing.
