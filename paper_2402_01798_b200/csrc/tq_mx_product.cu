@@ -84,6 +84,8 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[N]) {
     for (int i = 0; i < N; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// A map itself, ahead of its first use: it is a kernel parameter.
+__device__ __forceinline__ void fetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // A tile of a tensor map into this block's shared memory; x in bytes, a multiple of 16.
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -133,7 +135,7 @@ struct ProductArgs {
     uint64_t a_band, b0_band, b1_band;                           // bytes between 128 rows
     uint32_t m, n, k;                                            // n: columns of C, or features
     uint32_t tiles_m, tiles_n;
-    uint32_t a_rows;                                             // rows of A in a box (small kernel)
+    uint32_t a_rows;                                             // rows of A in a box
     void* out;                                                   // C, or the two projections (may be null)
     uint64_t out_stride;
     uint32_t out_bf16, out_wide;                                 // rows start on boundaries of this many bytes: 32, 16 or 0 for fewer
@@ -262,6 +264,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
         for (int s = 0; s < kPairStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1); mbar_init(drained, 16); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 32 * 9) {
+        fetch_map(&map_a); fetch_map(&map_b0); fetch_map(&maps.a); fetch_map(&maps.b0);
+        if constexpr (GATED != 0) { fetch_map(&map_b1); fetch_map(&maps.b1); }
     }
     __syncwarp();
     if (warp == 1) tmem_alloc<true>(smem_addr(&tmem_base), 512);
@@ -402,26 +408,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
 }
 
 // ---- small results ------------------------------------------------------------------------------------------------------
-// Where there are too few 256 x 256 tiles for the GPU (single tokens, short prompts): tiles of 128 rows of A and 128 rows of B (GATED: of each of
+// Where there are too few 256 x 256 tiles for the GPU (short prompts): tiles of 128 rows of A and 128 rows of B (GATED: of each of
 // the two matrices), one for a cluster of `split` blocks that share its columns k.  A slice of the tile's columns belongs to each block.  When all have
 // multiplied, every block sends the others their slices of its fp32 sums (remote stores wait for nothing) and keeps its own in registers, and
 // each adds up its slice in the order of the blocks.
-// Of A only as many rows as there are tokens are loaded, and stages are smaller and more for it: the multiplication reads 128 rows of whatever lies
-// there, and nobody reads the rows of the result that come from it.
 constexpr int kSplitThreads = 320;
 template <int GATED>
 struct SplitShape {
     static constexpr uint32_t kN = GATED ? 256 : 128;
     static constexpr uint32_t kCodesA = 128 * kBK / 2, kCodesB = kN * kBK / 2, kScaleBytes = 1024 + (GATED ? 2048 : 1024);
-    static constexpr uint32_t kMostStages = 8;
+    static constexpr uint32_t kStage = kCodesA + kCodesB + kScaleBytes, kStages = GATED ? 4 : 6;
     static constexpr uint32_t kScales = kN, kScaleColumns = 8 + kN / 16;          // columns of tensor memory
     static constexpr uint32_t kColumns = GATED ? 512 : 256;
-    static constexpr uint32_t kMostStageSmem = 208 * 1024;
-    static_assert(kScales + kMostStages * kScaleColumns <= kColumns, "");
-    // rows of A in a box -> bytes of a stage (boxes start on 1024 bytes), stages, and the whole allocation, in which 128 rows from the last box on stay
-    __host__ __device__ static uint32_t stage(uint32_t a_rows) { return kCodesB + (a_rows * 128 + kScaleBytes + 1023) / 1024 * 1024; }
-    static uint32_t stages(uint32_t a_rows) { return kMostStageSmem / stage(a_rows) < kMostStages ? kMostStageSmem / stage(a_rows) : kMostStages; }
+    static_assert(kScales + kStages * kScaleColumns <= kColumns, "");
 };
+
 // What a block receives from another one: for either half of its slice (a gated block: of 32 features, g and then u), four columns after four columns,
 // 16 bytes for each row.  A warp, which holds 32 rows, then sends 512 bytes in a piece (in pieces of 16 bytes, row after row, it took 2 us more a tile).
 template <int GATED, int SPLIT>
@@ -432,38 +433,34 @@ struct SplitSums {
     static constexpr uint32_t kRowBytes = kWidth * 4 * (GATED ? 2 : 1);
 };
 
-// The bytes of 8 codes are in lanes 0, 8, 16 and 24: one element a thread.
-__device__ __forceinline__ uint32_t e2m1_of_warp(float y) {
-    const float v[8] = {y, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    const uint32_t lane = threadIdx.x & 31;
-    return __reduce_or_sync(0xFFu << (lane & 24), e2m1_nearest8(v) << (4 * (lane & 7)));
-}
-__device__ __forceinline__ float load_shared(uint32_t addr) { float v; asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory"); return v; }
 __device__ __forceinline__ float4 load_shared4(uint32_t addr) {
     float4 v; asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory"); return v;
 }
 
 template <int GATED, int SPLIT>
 __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0,
-                                                                    const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ ProductArgs p, uint32_t stages,
-                                                                    uint32_t stage_bytes) {
+                                                                    const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ ProductArgs p, uint32_t stages) {
     using S = SplitShape<GATED>;
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
     __shared__ uint32_t tmem_base;
-    __shared__ __align__(8) uint64_t barriers[2 * S::kMostStages + 2];
+    __shared__ __align__(8) uint64_t barriers[2 * S::kStages + 2];
     __shared__ float scratch[8][kScratchWords];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
     const uint32_t bars = smem_addr(barriers);
     const auto full = [&](uint32_t s) { return bars + 8 * s; };
-    const auto empty = [&](uint32_t s) { return bars + 8 * (S::kMostStages + s); };
-    const uint32_t done = bars + 8 * (2 * S::kMostStages), flushed = done + 8;
+    const auto empty = [&](uint32_t s) { return bars + 8 * (S::kStages + s); };
+    const uint32_t done = bars + 8 * (2 * S::kStages), flushed = done + 8;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         dead = 0;
         for (uint32_t s = 0; s < stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 32 * 9) {
+        fetch_map(&map_a); fetch_map(&map_b0);
+        if constexpr (GATED != 0) fetch_map(&map_b1);
     }
     __syncwarp();
     if (warp == 1) tmem_alloc<false>(smem_addr(&tmem_base), S::kColumns);
@@ -476,7 +473,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     const uint32_t tm = tile % p.tiles_m, n0 = tile / p.tiles_m * 128;
     const uint32_t chunks = (p.k + kBK - 1) / kBK;
     const uint32_t first = chunks * rank / SPLIT, last = chunks * (rank + 1) / SPLIT;       // at least one: SPLIT <= chunks
-    const uint32_t at_a = S::kCodesB, at_scales = S::kCodesB + p.a_rows * 128;              // within a stage
+    constexpr uint32_t at_a = S::kCodesB, at_scales = S::kCodesB + S::kCodesA;              // within a stage
 
     if (warp == 0) {
         const bool leader = elect();
@@ -485,9 +482,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
         for (uint32_t c = first; c < last; ++c, ++it) {
             if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead))) break;
             if (leader) {
-                const uint32_t at = base + s * stage_bytes, scales = at + at_scales;
+                const uint32_t at = base + s * S::kStage, scales = at + at_scales;
                 const uint32_t bytes = (p.k + 127) / 128 - 2 * c < 2 ? 512 : 1024;
-                mbar_expect_tx(full(s), p.a_rows * 128 + S::kCodesB + bytes * (GATED ? 3 : 2));
+                mbar_expect_tx(full(s), S::kCodesA + S::kCodesB + bytes * (GATED ? 3 : 2));
                 tma_load(at, &map_b0, c * (kBK / 2), n0, full(s));
                 if constexpr (GATED != 0) tma_load(at + S::kCodesB / 2, &map_b1, c * (kBK / 2), n0, full(s));
                 tma_load(at + at_a, &map_a, c * (kBK / 2), tm * 128, full(s));
@@ -506,7 +503,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
         const uint32_t n = GATED ? 256 : p.n - n0 < 128 ? (p.n - n0 + 15) / 16 * 16 : 128;
         const uint32_t last_steps = (p.k - (chunks - 1) * kBK + 63) / 64;
         const auto copy_stage = [&](uint32_t s) {                // of a chunk with one tile of scales the second is whatever lies there, and no step takes it
-            const uint32_t scales = base + s * stage_bytes + at_scales, to = tmem + S::kScales + s * S::kScaleColumns;
+            const uint32_t scales = base + s * S::kStage + at_scales, to = tmem + S::kScales + s * S::kScaleColumns;
 #pragma unroll
             for (uint32_t j = 0; j < 2; ++j) {
                 copy_scales<false>(to + 4 * j, scale_desc(scales + 512 * j));
@@ -520,7 +517,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
             if (!(ok = warp_wait(full(s), round & 1, &dead))) break;
             fence_after();
             if (leader) {
-                const uint32_t at = base + s * stage_bytes;
+                const uint32_t at = base + s * S::kStage;
                 const uint32_t scale_a = tmem + S::kScales + s * S::kScaleColumns, scale_b = scale_a + 8;
                 const uint32_t steps = c + 1 < chunks ? 4 : last_steps;
                 const uint64_t a = operand_desc(at + at_a), b = operand_desc(at);
@@ -587,8 +584,6 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     } else {
         using Q = SplitSums<GATED, SPLIT>;
         const uint32_t part = rows * Q::kRowBytes, quad = rows * 16;                 // bytes from one half, or four columns, to the next
-        // Few rows of a gated block: a warp makes 32 elements, a thread one of them, and its own sums go through shared memory as well.
-        const bool few = GATED && rows * Q::kHalves <= 16;
         const auto received = [&](uint32_t b, uint32_t h, uint32_t r) { return base + (b * Q::kHalves + h) * part + r * 16; };
         const auto send = [&](uint32_t owner, uint32_t h) {
             float v[Q::kWidth];
@@ -610,45 +605,14 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
 #pragma unroll 1
             for (uint32_t i = 0; i < SPLIT; ++i) {
                 const uint32_t owner = (rank + 1 + i) % SPLIT;
-                if (owner == rank && !few) continue;
+                if (owner == rank) continue;
                 if (Q::kHalves == 2) send(owner, half);
                 else if ((i & 1) == half) send(owner, 0);
             }
         }
         __syncthreads();
         cluster_sync();
-        if (few) {
-            for (uint32_t item = warp; item < rows * Q::kHalves; item += kSplitThreads / 32) {
-                const uint32_t r = item / Q::kHalves, h = item % Q::kHalves, j = rank * Q::kHalves + h, f = n0 + 32 * j;
-                uint32_t byte = 0;
-                if (f < p.n) {
-                    float g = 0.0f, u = 0.0f;
-#pragma unroll
-                    for (uint32_t b = 0; b < SPLIT; ++b) {
-                        const uint32_t at = received(b, h, r) + lane / 4 * quad + lane % 4 * 4;
-                        g += load_shared(at); u += load_shared(at + 8 * quad);
-                    }
-                    const uint64_t to_row = tm * 128 + r;
-                    if (p.out) {
-                        const uint64_t to = to_row * p.out_stride + f + lane;
-                        if (p.out_bf16) {
-                            static_cast<unsigned short*>(p.out)[to] = static_cast<unsigned short>(pack_bf16(g, 0.0f));
-                            static_cast<unsigned short*>(p.out)[to + p.n] = static_cast<unsigned short>(pack_bf16(u, 0.0f));
-                        } else {
-                            static_cast<float*>(p.out)[to] = g;
-                            static_cast<float*>(p.out)[to + p.n] = u;
-                        }
-                    }
-                    const float x = gate_value<GATED == 2>(g) * u;
-                    // a NaN's pattern without its sign is above infinity's, and that above all others
-                    byte = mx_scale_byte<false>(__uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x) & 0x7FFFFFFFu)));
-                    const uint32_t codes = e2m1_of_warp(x * mx_inv_scale(byte));
-                    if ((lane & 7) == 0)
-                        asm volatile("st.global.b32 [%0], %1;" ::"l"(p.h.codes + to_row * p.h.code_stride + f / 2 + lane / 2), "r"(byte == 255u ? 0u : codes) : "memory");
-                }
-                if (lane == 0) put_scale(r, j, byte);
-            }
-        } else if (taker && fine && half < Q::kHalves) {
+        if (taker && fine && half < Q::kHalves) {
             const uint32_t col = n0 + rank * Q::kSlice + half * Q::kWidth;
             float v[Q::kWidth];
             const auto add_up = [&](float (&x)[Q::kWidth], uint32_t first_quad) {        // what the own block has in x with the others', in their order
@@ -687,6 +651,237 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     if (warp == 1) tmem_free<false>(tmem, S::kColumns);
 }
 
+// ---- few rows of A: single tokens ------------------------------------------------------------------------------------------
+// Up to 64 rows of A are the narrow operand here: a multiplication of 128 rows of B by 8 to 64 rows of A, k shared by a cluster of SPLIT blocks.  What counts is
+// that every SM reads B as fast as it can: with A's rows on the wide side, four multiplications of 128 x 128 x 64 and their scales took 540 clocks for
+// 16 KB of B (1 x 8192 x 8192 read 2.5 TB/s).  Two blocks an SM, so that one loads while the other starts or ends.
+// A thread of the epilogue has one column of C, or feature, for all rows; 32 features of a row are a warp's, and so is their block of h.
+constexpr uint32_t kMostTokens = 64;
+constexpr uint32_t kMostGatedTokens = 16;                        // beyond, the activation of one row after another takes too long (64 x 2048 x 16384: 15 us, split blocks 7)
+template <int GATED>
+struct TokenShape {
+    static constexpr uint32_t kCodesB = (GATED ? 256 : 128) * kBK / 2, kScaleBytes = GATED ? 3072 : 2048;
+    static constexpr uint32_t kMostStages = GATED ? 5 : 8, kMostSmem = 108 * 1024;
+    static constexpr uint32_t kScales = 128, kScaleColumns = GATED ? 24 : 16, kColumns = 256;       // of tensor memory; sums in the first 128
+    static_assert(kScales + kMostStages * kScaleColumns <= kColumns, "");
+    __host__ __device__ static uint32_t stage(uint32_t a_rows) { return kCodesB + a_rows * 128 + kScaleBytes; }
+};
+
+// The bytes of 8 codes are in lanes 0, 8, 16 and 24: one element a thread.
+__device__ __forceinline__ uint32_t e2m1_of_warp(float y) {
+    const float v[8] = {y, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t lane = threadIdx.x & 31;
+    return __reduce_or_sync(0xFFu << (lane & 24), e2m1_nearest8(v) << (4 * (lane & 7)));
+}
+__device__ __forceinline__ float load_shared(uint32_t addr) { float v; asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory"); return v; }
+__device__ __forceinline__ void store_one(const ProductArgs& p, uint64_t at, float x) {
+    if (p.out_bf16) static_cast<unsigned short*>(p.out)[at] = static_cast<unsigned short>(pack_bf16(x, 0.0f));
+    else static_cast<float*>(p.out)[at] = x;
+}
+// Row r, 32 features from f on, one a thread.
+template <bool GELU>
+__device__ __forceinline__ void store_gated_warp(const ProductArgs& p, uint32_t r, uint32_t f, float g, float u) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (f >= p.n) return;
+    if (p.out) {
+        store_one(p, r * p.out_stride + f + lane, g);
+        store_one(p, r * p.out_stride + p.n + f + lane, u);
+    }
+    const float x = gate_value<GELU>(g) * u;
+    // a NaN's pattern without its sign is above infinity's, and that above all others
+    const uint32_t byte = mx_scale_byte<false>(__uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x) & 0x7FFFFFFFu)));
+    const uint32_t codes = e2m1_of_warp(x * mx_inv_scale(byte));
+    if ((lane & 7) == 0)
+        asm volatile("st.global.b32 [%0], %1;" ::"l"(p.h.codes + r * p.h.code_stride + f / 2 + lane / 2), "r"(byte == 255u ? 0u : codes) : "memory");
+    if (lane == 0) p.h.scales[mx_scale_at(p.h, r, f / 32)] = static_cast<uint8_t>(byte);
+}
+
+template <int GATED, int SPLIT>
+__global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0,
+                                                                    const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ ProductArgs p, uint32_t stages) {
+    using S = TokenShape<GATED>;
+    constexpr int kSums = GATED ? 2 : 1;
+    extern __shared__ unsigned char raw[];
+    __shared__ volatile int dead;
+    __shared__ uint32_t tmem_base;
+    __shared__ __align__(8) uint64_t barriers[2 * S::kMostStages + 2];
+    const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t bars = smem_addr(barriers);
+    const auto full = [&](uint32_t s) { return bars + 8 * s; };
+    const auto empty = [&](uint32_t s) { return bars + 8 * (S::kMostStages + s); };
+    const uint32_t done = bars + 8 * (2 * S::kMostStages), flushed = done + 8;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        dead = 0;
+        for (uint32_t s = 0; s < stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        mbar_init(done, 1); mbar_init(flushed, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 32 * 9) {
+        fetch_map(&map_a); fetch_map(&map_b0);
+        if constexpr (GATED != 0) fetch_map(&map_b1);
+    }
+    __syncwarp();
+    if (warp == 1) tmem_alloc<false>(smem_addr(&tmem_base), S::kColumns);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    pdl_wait();
+    const uint32_t tmem = tmem_base;
+    const uint32_t rank = blockIdx.x % SPLIT, n0 = blockIdx.x / SPLIT * 128;
+    const uint32_t chunks = (p.k + kBK - 1) / kBK;
+    const uint32_t first = chunks * rank / SPLIT, last = chunks * (rank + 1) / SPLIT;       // at least one: SPLIT <= chunks
+    const uint32_t stage_bytes = S::stage(p.a_rows), at_scales = S::kCodesB + p.a_rows * 128;     // scales of A, B and B's second matrix
+
+    if (warp == 0) {
+        const bool leader = elect();
+        uint32_t s = 0, round = 0, it = 0;
+        bool ok = true;
+        for (uint32_t c = first; c < last; ++c, ++it) {
+            if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead))) break;
+            if (leader) {
+                const uint32_t at = base + s * stage_bytes, scales = at + at_scales;
+                const uint32_t bytes = (p.k + 127) / 128 - 2 * c < 2 ? 512 : 1024;
+                mbar_expect_tx(full(s), S::kCodesB + p.a_rows * 128 + bytes * (1 + kSums));
+                tma_load(at, &map_b0, c * (kBK / 2), n0, full(s));
+                if constexpr (GATED != 0) tma_load(at + S::kCodesB / 2, &map_b1, c * (kBK / 2), n0, full(s));
+                bulk_load(scales + 1024, p.b0_scales + (n0 / 128) * p.b0_band + c * 1024ull, bytes, full(s));
+                if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024ull, bytes, full(s));
+                tma_load(at + S::kCodesB, &map_a, c * (kBK / 2), 0, full(s));
+                bulk_load(scales, p.a_scales + c * 1024ull, bytes, full(s));
+            }
+            __syncwarp();
+            if (++s == stages) { s = 0; ++round; }
+        }
+        if (!ok && leader)                                       // nothing may still be on its way into a block that ends
+            for (uint32_t j = it > stages ? it - stages : 0; j < it; ++j) mbar_wait(full(j % stages), (j / stages) & 1);
+        __syncwarp();
+    } else if (warp == 1) {
+        const bool leader = elect();
+        const uint32_t last_steps = (p.k - (chunks - 1) * kBK + 63) / 64;
+        uint32_t s = 0, round = 0;
+        bool ok = true;
+        for (uint32_t c = first; c < last; ++c) {
+            if (!(ok = warp_wait(full(s), round & 1, &dead))) break;
+            fence_after();
+            if (leader) {
+                const uint32_t at = base + s * stage_bytes, scales = at + at_scales;
+                const uint32_t columns = tmem + S::kScales + s * S::kScaleColumns;           // 2 x 4 of A, 2 x 4 of B, 2 x 4 of B's second matrix
+                const uint32_t steps = c + 1 < chunks ? 4 : last_steps;
+                const uint64_t a = operand_desc(at + S::kCodesB), b = operand_desc(at), b1 = operand_desc(at + S::kCodesB / 2);
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j)                 // of a chunk with one tile of scales the second is whatever lies there, and no step takes it
+#pragma unroll
+                    for (uint32_t w = 0; w < 1 + kSums; ++w) copy_scales<false>(columns + 8 * w + 4 * j, scale_desc(scales + 1024 * w + 512 * j));
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)                 // 64 elements, 32 bytes, are 2 in the address field
+                    if (i < steps) {
+                        const uint32_t idesc = mxf4_desc(128, p.a_rows, (i & 1) * 2), more = (c != first) | (i != 0);
+                        mma_mxf4<false>(tmem, b + 2 * i, a + 2 * i, idesc, columns + 8 + 4 * (i >> 1), columns + 4 * (i >> 1), more);
+                        if constexpr (GATED != 0) mma_mxf4<false>(tmem + kMostTokens, b1 + 2 * i, a + 2 * i, idesc, columns + 16 + 4 * (i >> 1), columns + 4 * (i >> 1), more);
+                    }
+                mma_commit<false>(empty(s));
+            }
+            __syncwarp();
+            if (++s == stages) { s = 0; ++round; }
+        }
+        if (leader) {
+            if (ok) mma_commit<false>(done);
+            else {                                               // let the multiplications that were issued come to an end
+                mma_commit<false>(flushed);
+                mbar_wait(flushed, 0);
+            }
+        }
+        __syncwarp();
+    }
+    // Two warps for each quarter of the lanes, 32 columns or features: they take eight rows in turn.
+    const uint32_t quarter = warp % 4, half = (warp - 2) / 4;
+    const uint32_t from = tmem + ((quarter * 32) << 16);
+    bool fine = true;
+    if (warp >= 2) {
+        fine = warp_wait(done, 0, &dead);
+        fence_after();
+    }
+    if constexpr (GATED != 0) {
+        // the scales' tile is written for all 128 rows, those behind the last token with zeros
+        for (uint32_t item = threadIdx.x; item < (128 - p.m) * (4 / SPLIT); item += kSplitThreads) {
+            const uint32_t r = p.m + item / (4 / SPLIT), j = rank * (4 / SPLIT) + item % (4 / SPLIT);
+            p.h.scales[(n0 / 128) * 512 + (r % 32) * 16 + (r / 32) * 4 + j] = 0;
+        }
+        // and where the features end inside it, the blocks behind them as well
+        for (uint32_t item = threadIdx.x; item < p.m * (4 / SPLIT); item += kSplitThreads) {
+            const uint32_t r = item / (4 / SPLIT), j = rank * (4 / SPLIT) + item % (4 / SPLIT);
+            if (n0 + 32 * j >= p.n) p.h.scales[(n0 / 128) * 512 + (r % 32) * 16 + (r / 32) * 4 + j] = 0;
+        }
+    }
+    if constexpr (SPLIT == 1) {
+        if (warp >= 2 && fine) {
+#pragma unroll 1
+            for (uint32_t r0 = 8 * half; r0 < p.m; r0 += 16) {
+                float v[8], u[8];
+                tmem_load(from + r0, v);
+                if constexpr (GATED != 0) tmem_load(from + kMostTokens + r0, u);
+                tmem_wait_loads();
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) {
+                    if (r0 + i >= p.m) break;
+                    if constexpr (GATED != 0) store_gated_warp<GATED == 2>(p, r0 + i, n0 + 32 * quarter, v[i], u[i]);
+                    else if (n0 + 32 * quarter + lane < p.n) store_one(p, (r0 + i) * p.out_stride + n0 + 32 * quarter + lane, v[i]);
+                }
+                __syncwarp();
+            }
+        }
+    } else {
+        constexpr uint32_t kSlice = 128 / SPLIT;                 // columns or features of a block
+        // what a block receives: from each block, for each row, its slice of g (or C) and of u
+        const auto place = [&](uint32_t b, uint32_t r, uint32_t w, uint32_t col) { return base + (((b * p.m + r) * kSums + w) * kSlice + col) * 4; };
+        __syncthreads();
+        cluster_sync();                                          // all blocks have multiplied: the stages are free
+        if (warp >= 2 && fine) {
+            const uint32_t col = quarter * 32 + lane, owner = col / kSlice;
+#pragma unroll 1
+            for (uint32_t r0 = 8 * half; r0 < p.m; r0 += 16) {
+#pragma unroll
+                for (uint32_t w = 0; w < kSums; ++w) {
+                    float v[8];
+                    tmem_load(from + kMostTokens * w + r0, v);
+                    tmem_wait_loads();
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i)
+                        if (r0 + i < p.m) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(of_rank(place(rank, r0 + i, w, col % kSlice), owner)), "f"(v[i]) : "memory");
+                    __syncwarp();
+                }
+            }
+        }
+        __syncthreads();
+        cluster_sync();
+        if constexpr (GATED != 0) {
+            constexpr uint32_t kBlocks = kSlice / 32;            // SPLIT is 2 or 4
+            for (uint32_t item = warp; item < p.m * kBlocks; item += kSplitThreads / 32) {
+                const uint32_t r = item / kBlocks, j = item % kBlocks;
+                float g = 0.0f, u = 0.0f;
+#pragma unroll
+                for (uint32_t b = 0; b < SPLIT; ++b) { g += load_shared(place(b, r, 0, 32 * j + lane)); u += load_shared(place(b, r, 1, 32 * j + lane)); }
+                store_gated_warp<GATED == 2>(p, r, n0 + rank * kSlice + 32 * j, g, u);
+            }
+        } else {
+            for (uint32_t item = threadIdx.x; item < p.m * kSlice; item += kSplitThreads) {
+                const uint32_t r = item / kSlice, col = n0 + rank * kSlice + item % kSlice;
+                float x = 0.0f;
+#pragma unroll
+                for (uint32_t b = 0; b < SPLIT; ++b) x += load_shared(place(b, r, 0, item % kSlice));
+                if (col < p.n) store_one(p, r * p.out_stride + col, x);
+            }
+        }
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && dead) atomicAdd(&g_product_wait_expired, 1u);
+    fence_after();
+    if (warp == 1) tmem_free<false>(tmem, S::kColumns);
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -711,39 +906,45 @@ cudaError_t codes_map(CUtensorMap* map, const tq_mx_t& m, uint32_t rows) {
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-// Memory of a split block: its stages, or what it receives.
-constexpr uint32_t kMostSplitSmem = 216 * 1024;                  // beside 10 KB of fixed arrays
-struct SplitMemory {
-    uint32_t stages, stage_bytes;
+// Shared memory of a block that waits in the tensor core's allocator while its cluster waits for it: no more of them on an SM than its tensor memory serves at once,
+// or two clusters that hold each other's columns would wait for ever.  Blocks with 256 columns ask for more than a third of an SM's memory, so that two
+// fit; those with 512 for so much that nothing of the kind fits beside them.
+constexpr size_t kLeastHalf = 77 * 1024, kLeastWhole = 160 * 1024;
+struct BlockMemory {
+    uint32_t stages;
     size_t bytes;
 };
+inline size_t at_least(size_t need, size_t least) { return need > least ? need : least; }
 template <int GATED>
-SplitMemory split_memory(uint32_t rows, uint32_t a_rows, uint64_t chunks, uint32_t split) {
+BlockMemory split_memory(uint32_t rows, uint64_t chunks, uint32_t split) {
     using S = SplitShape<GATED>;
-    SplitMemory m{S::stages(a_rows), S::stage(a_rows), 0};
     const uint64_t most = (chunks + split - 1) / split;
-    if (m.stages > most) m.stages = static_cast<uint32_t>(most);
-    const uint32_t sums = split > 1 ? rows * 128 * 4 * (GATED ? 2 : 1) : 0;
-    const uint32_t last = S::kCodesA > m.stage_bytes - S::kCodesB ? S::kCodesA : m.stage_bytes - S::kCodesB;      // 128 rows of A from the last box on
-    while ((m.stages - 1) * m.stage_bytes + S::kCodesB + last + 1024 > kMostSplitSmem) --m.stages;
-    const uint32_t staged = (m.stages - 1) * m.stage_bytes + S::kCodesB + last;
-    // No more blocks on an SM than its tensor memory serves at once, two plain ones, or one gated one and nothing beside it: a block that waits for
-    // columns keeps its cluster waiting, and two clusters that hold each other's columns would wait for ever.
-    const size_t least = GATED ? 160 * 1024 : 77 * 1024, need = (staged > sums ? staged : sums) + 1024;
-    m.bytes = need > least ? need : least;
-    return m;
+    const uint32_t stages = most < S::kStages ? static_cast<uint32_t>(most) : S::kStages, sums = split > 1 ? rows * 128 * 4 * (GATED ? 2 : 1) : 0;
+    const uint32_t staged = stages * S::kStage;
+    return BlockMemory{stages, at_least((staged > sums ? staged : sums) + 1024, GATED ? kLeastWhole : kLeastHalf)};
 }
+template <int GATED>
+BlockMemory token_memory(uint32_t rows, uint32_t a_rows, uint64_t chunks, uint32_t split) {
+    using S = TokenShape<GATED>;
+    const uint64_t most = (chunks + split - 1) / split;
+    uint32_t stages = S::kMostSmem / S::stage(a_rows);
+    if (stages > S::kMostStages) stages = S::kMostStages;
+    if (stages > most) stages = static_cast<uint32_t>(most);
+    const uint32_t staged = stages * S::stage(a_rows), sums = split > 1 ? rows * 128 * 4 * (GATED ? 2 : 1) : 0;
+    return BlockMemory{stages, at_least((staged > sums ? staged : sums) + 1024, kLeastHalf)};
+}
+constexpr size_t kMostSplitSmem = 212 * 1024, kMostTokenSmem = 109 * 1024;        // of any call, beside a few KB of fixed arrays
 
 // Which kernel, and how many blocks share a tile: by an estimate of the time in ns, fitted to graphs of 20 launches.  A pair takes 430 a stage and 1300 a
-// tile at least; a split block 285 (two B matrices: 340) and up to 70 more as A's rows and the busy SMs grow.  Adding up costs 1 us and 4 ns for each row and block.
-// Measured (pair / split 1 / 2 / 4 / 8): 1 x 8192 x 4096 9.9 / 7.1 / 6.0 / 5.6 / 9.7 us, 777 x 1000 x 4000 12.6 / 10.3 / 8.9 / 14 / 17,
-// 1024 x 2048 x 4096 9.9 / 8.4 / 14 / 24 / 33, 2048^3 8.2 / 11 / 23 / 30 / 59, gated 4 x 4096 x 8192 12 / 9.2 / 7.4 / 11, gated 512 x 4096 x 8192 17 / 19 / 36 / 71.
+// tile at least; a split block 310 (two B matrices: 365) and up to 70 more as the SMs fill.  Adding up costs 1 us and 4 ns for each row and block.
+// Measured (pair / split 1 / 2 / 4 / 8): 777 x 1000 x 4000 12.6 / 10.3 / 8.9 / 14 / 17 us, 1024 x 2048 x 4096 9.9 / 8.4 / 14 / 24 / 33, 2048^3 8.2 / 11 / 23 / 30 / 59,
+// 128 x 4096 x 4096 9.8 / 7.8 / 7.2 / 6.4 / 9.0, gated 512 x 4096 x 8192 17 / 19 / 36 / 71.
 struct ProductPlan {
     bool pair;
     uint32_t split;
 };
 template <int GATED>
-ProductPlan plan_product(uint32_t m, uint32_t n, uint32_t k, uint32_t a_rows) {
+ProductPlan plan_product(uint32_t m, uint32_t n, uint32_t k) {
     const uint64_t sms = static_cast<uint64_t>(sm_count()), chunks = (static_cast<uint64_t>(k) + kBK - 1) / kBK;
     const uint64_t wide = (static_cast<uint64_t>(m) + 255) / 256 * ((static_cast<uint64_t>(n) + (GATED ? 127 : 255)) / (GATED ? 128 : 256)), pairs = sms / 2;
     const uint64_t tile = chunks * 430 > 1300 ? chunks * 430 : 1300;
@@ -752,15 +953,21 @@ ProductPlan plan_product(uint32_t m, uint32_t n, uint32_t k, uint32_t a_rows) {
     const uint64_t narrow = (static_cast<uint64_t>(m) + 127) / 128 * ((static_cast<uint64_t>(n) + 127) / 128);
     const uint32_t rows = m < 128 ? m : 128;
     for (uint32_t split = 1; split <= (GATED ? 4u : 8u) && split <= chunks; split *= 2) {
-        // two blocks of few rows run side by side on an SM; two with all rows take as long as one after the other (4096 x 1024 x 250: 7.0 us, a pair 5.9)
-        const bool two = !GATED && rows <= 32 && split_memory<GATED>(rows, a_rows, chunks, split).bytes <= 100 * 1024;      // beside 10 KB of fixed arrays
-        const uint64_t room = (split == 8 ? sms * 7 / 8 : sms) * (two ? 2 : 1), blocks = narrow * split;
-        const uint64_t waves = (blocks + room - 1) / room, stage = (GATED ? 340 : 285) + rows / 5 + 70 * (blocks < sms ? blocks : sms) / sms;
+        const uint64_t room = split == 8 ? sms * 7 / 8 : sms, blocks = narrow * split;
+        const uint64_t waves = (blocks + room - 1) / room, stage = (GATED ? 365 : 310) + 70 * (blocks < sms ? blocks : sms) / sms;
         const uint64_t sums = split == 1 ? 500 : 800 + 100 * split + 4 * rows * split;
         const uint64_t cost = 2600 + waves * ((chunks + split - 1) / split * stage + sums) + (waves - 1) * 1500;
         if (cost < best) { best = cost; plan = ProductPlan{false, split}; }
     }
     return plan;
+}
+// Blocks a tile for few rows: as many as fit on the GPU at once, two on an SM, while each has two stages at least.
+template <int GATED>
+uint32_t plan_tokens(uint32_t n, uint32_t k) {
+    const uint64_t tiles = (static_cast<uint64_t>(n) + 127) / 128, chunks = (static_cast<uint64_t>(k) + kBK - 1) / kBK, room = 2 * static_cast<uint64_t>(sm_count());
+    uint32_t split = 1;
+    while (split < (GATED ? 4u : 8u) && tiles * split * 2 <= room && chunks >= split * 4) split *= 2;
+    return split;
 }
 
 // `most`: of shared memory, for any call
@@ -789,12 +996,21 @@ cudaError_t scales_map(CUtensorMap* map, const tq_mx_t& m) {
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int GATED, int SPLIT>
+template <int GATED, int SPLIT, bool TOKENS>
 cudaError_t launch_split_as(const CUtensorMap& map_a, const CUtensorMap& map_b0, const CUtensorMap& map_b1, const ProductArgs& p, cudaStream_t stream) {
-    using S = SplitShape<GATED>;
-    SplitMemory mem = split_memory<GATED>(p.m < 128 ? p.m : 128, p.a_rows, (static_cast<uint64_t>(p.k) + kBK - 1) / kBK, SPLIT);
-    void* args[] = {const_cast<CUtensorMap*>(&map_a), const_cast<CUtensorMap*>(&map_b0), const_cast<CUtensorMap*>(&map_b1), const_cast<ProductArgs*>(&p), &mem.stages, &mem.stage_bytes};
-    return launch_clustered<mx_split_kernel<GATED, SPLIT>>(p.tiles_m * p.tiles_n * SPLIT, SPLIT, kSplitThreads, mem.bytes, kMostSplitSmem, stream, args);
+    const uint64_t chunks = (static_cast<uint64_t>(p.k) + kBK - 1) / kBK;
+    BlockMemory mem = TOKENS ? token_memory<GATED>(p.m, p.a_rows, chunks, SPLIT) : split_memory<GATED>(p.m < 128 ? p.m : 128, chunks, SPLIT);
+    void* args[] = {const_cast<CUtensorMap*>(&map_a), const_cast<CUtensorMap*>(&map_b0), const_cast<CUtensorMap*>(&map_b1), const_cast<ProductArgs*>(&p), &mem.stages};
+    const unsigned blocks = p.tiles_m * p.tiles_n * SPLIT;
+    if constexpr (TOKENS) return launch_clustered<mx_token_kernel<GATED, SPLIT>>(blocks, SPLIT, kSplitThreads, mem.bytes, kMostTokenSmem, stream, args);
+    else return launch_clustered<mx_split_kernel<GATED, SPLIT>>(blocks, SPLIT, kSplitThreads, mem.bytes, kMostSplitSmem, stream, args);
+}
+template <int GATED, bool TOKENS>
+cudaError_t launch_split(uint32_t split, const CUtensorMap& map_a, const CUtensorMap& map_b0, const CUtensorMap& map_b1, const ProductArgs& p, cudaStream_t stream) {
+    if (split == 2) return launch_split_as<GATED, 2, TOKENS>(map_a, map_b0, map_b1, p, stream);
+    if (split == 4) return launch_split_as<GATED, 4, TOKENS>(map_a, map_b0, map_b1, p, stream);
+    if constexpr (!GATED) if (split == 8) return launch_split_as<0, 8, TOKENS>(map_a, map_b0, map_b1, p, stream);
+    return launch_split_as<GATED, 1, TOKENS>(map_a, map_b0, map_b1, p, stream);
 }
 
 template <int GATED>
@@ -805,9 +1021,9 @@ cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t
     p.m = static_cast<uint32_t>(a.rows); p.n = static_cast<uint32_t>(b0.rows); p.k = static_cast<uint32_t>(a.cols);
     const uint64_t at = reinterpret_cast<uintptr_t>(p.out) | (p.m > 1 ? p.out_stride * (p.out_bf16 ? 2 : 4) : 0) | (GATED ? p.n * (p.out_bf16 ? 2 : 4) : 0);
     p.out_wide = at % 32 == 0 ? 32 : at % 16 == 0 ? 16 : 0;
-    const uint32_t few = p.m >= 128 ? 128 : (p.m + 7) / 8 * 8;
-    const ProductPlan plan = plan_product<GATED>(p.m, p.n, p.k, few);
-    p.a_rows = plan.pair ? 128 : few;
+    const bool tokens = p.m <= (GATED ? kMostGatedTokens : kMostTokens);
+    const ProductPlan plan = tokens ? ProductPlan{false, plan_tokens<GATED>(p.n, p.k)} : plan_product<GATED>(p.m, p.n, p.k);
+    p.a_rows = tokens ? (p.m + 7) / 8 * 8 : 128;
     CUtensorMap map_a, map_b0, map_b1;
     if (const cudaError_t e = codes_map(&map_a, a, p.a_rows)) return e;
     if (const cudaError_t e = codes_map(&map_b0, b0, 128)) return e;
@@ -827,10 +1043,7 @@ cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t
         return launch_clustered<mx_pair_kernel<GATED>>(2 * (tiles < pairs ? tiles : pairs), 0, kPairThreads, kPairSmem, kPairSmem, stream, args);
     }
     p.tiles_m = (p.m + 127) / 128; p.tiles_n = (p.n + 127) / 128;
-    if (plan.split == 2) return launch_split_as<GATED, 2>(map_a, map_b0, map_b1, p, stream);
-    if (plan.split == 4) return launch_split_as<GATED, 4>(map_a, map_b0, map_b1, p, stream);
-    if constexpr (!GATED) if (plan.split == 8) return launch_split_as<0, 8>(map_a, map_b0, map_b1, p, stream);
-    return launch_split_as<GATED, 1>(map_a, map_b0, map_b1, p, stream);
+    return tokens ? launch_split<GATED, true>(plan.split, map_a, map_b0, map_b1, p, stream) : launch_split<GATED, false>(plan.split, map_a, map_b0, map_b1, p, stream);
 }
 
 }  // namespace
