@@ -429,7 +429,12 @@ class MxMatrix:
 
     def __init__(self, codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], rows: int, cols: int, layout: int = MX_TILES,
                  memory: Optional[torch.Tensor] = None):
-        self._codes, self._scales, self.rows, self.cols, self.layout, self.memory = codes, scales, rows, cols, layout, memory
+        self._codes = codes
+        self._scales = scales
+        self.rows = rows
+        self.cols = cols
+        self.layout = layout
+        self.memory = memory
 
     def _views(self):
         width, stride, at, scale_rows, scale_stride = _calls().mx_layout(self.rows, self.cols, self.layout)

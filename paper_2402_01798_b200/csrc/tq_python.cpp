@@ -384,7 +384,7 @@ tq_status decompress_aggregate_segments(Args& a) {           // packed, segments
 
 // ---- microscaled 4-bit floating point: an MxMatrix (binding.py) is six attributes ---------------------------------
 struct MxNames {
-    PyObject *codes, *scales, *rows, *cols, *layout, *memory, *own_codes, *own_scales;
+    PyObject *rows, *cols, *layout, *memory, *own_codes, *own_scales;
 } N;
 // A matrix in one piece of memory: codes, and on the next 128-byte boundary scales.  Rows of codes that are longer than 128 bytes start on such a
 // boundary: the products load 128 bytes of a row at a time.
@@ -449,8 +449,8 @@ tq_mx_t mx(PyObject* o) {
     }
     const uint64_t blocks = m.cols / 32 + (m.cols % 32 != 0);
     const bool tiles = m.layout == TQ_MX_TILES;
-    m.codes = bytes_of(o, N.codes, "codes", m.rows, blocks * 16, &m.code_stride);
-    m.scales = bytes_of(o, N.scales, "scales", tiles ? m.rows / 128 + (m.rows % 128 != 0) : m.rows, tiles ? (blocks + 3) / 4 * 512 : (blocks + 15) / 16 * 16, &m.scale_stride);
+    m.codes = bytes_of(o, N.own_codes, "codes", m.rows, blocks * 16, &m.code_stride);
+    m.scales = bytes_of(o, N.own_scales, "scales", tiles ? m.rows / 128 + (m.rows % 128 != 0) : m.rows, tiles ? (blocks + 3) / 4 * 512 : (blocks + 15) / 16 * 16, &m.scale_stride);
     return m;
 }
 // A plain [rows, cols] tensor, fp32 or bf16; a vector is one row.  At least `rows` x `cols` where those are given.
@@ -544,7 +544,7 @@ const at::Tensor& tensor_of(PyObject* matrix) {
     if (!v) throw Failed();
     Py_DECREF(v);                                                  // held by the matrix
     if (v == Py_None) {
-        v = PyObject_GetAttr(matrix, N.codes);
+        v = PyObject_GetAttr(matrix, N.own_codes);
         if (!v) throw Failed();
         Py_DECREF(v);
     }
@@ -715,9 +715,9 @@ PyModuleDef module{PyModuleDef_HEAD_INIT, "_tq_python", "Argument marshalling fo
 }  // namespace
 
 PyMODINIT_FUNC PyInit__tq_python() {
-    N = MxNames{PyUnicode_InternFromString("codes"), PyUnicode_InternFromString("scales"), PyUnicode_InternFromString("rows"), PyUnicode_InternFromString("cols"),
+    N = MxNames{PyUnicode_InternFromString("rows"), PyUnicode_InternFromString("cols"),
                 PyUnicode_InternFromString("layout"), PyUnicode_InternFromString("memory"),
                 PyUnicode_InternFromString("_codes"), PyUnicode_InternFromString("_scales")};
-    if (!N.codes || !N.scales || !N.rows || !N.cols || !N.layout || !N.memory || !N.own_codes || !N.own_scales) return nullptr;
+    if (!N.rows || !N.cols || !N.layout || !N.memory || !N.own_codes || !N.own_scales) return nullptr;
     return PyModule_Create(&module);
 }
