@@ -1038,7 +1038,9 @@ cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t
         ScaleMaps maps;
         if (const cudaError_t e = scales_map(&maps.a, a)) return e;
         if (const cudaError_t e = scales_map(&maps.b0, b0)) return e;
-        if (const cudaError_t e = scales_map(&maps.b1, b1)) return e;
+        maps.b1 = maps.b0;
+        if (GATED)
+            if (const cudaError_t e = scales_map(&maps.b1, b1)) return e;
         void* args[] = {&map_a, &map_b0, &map_b1, &maps, &p};
         return launch_clustered<mx_pair_kernel<GATED>>(2 * (tiles < pairs ? tiles : pairs), 0, kPairThreads, kPairSmem, kPairSmem, stream, args);
     }
