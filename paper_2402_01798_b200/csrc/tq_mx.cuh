@@ -69,8 +69,8 @@ __device__ __forceinline__ uint32_t e2m1_nearest8(const float (&v)[8]) {
 //     F(a) = 2a (a < 2),  a + 2 (2 <= a < 4),  a / 2 + 4 (4 <= a)  =  min(2a, a + 2, a / 2 + 4),
 // the code below it being floor F(a) and p the rest.  P = rint(2^16 F(a)) is the smallest of three fused multiply-adds onto a magic number (the
 // products are exact, each is rounded once to an integer, 2^17 and 2^18 are even, and rounding keeps the order).  The code is
-// (P + 65535 - r) >> 16, one up when r < rint(p 2^16): byte 2 of the sum.  (By the exponent of a: four operations of the integer pipe, here one; rows of
-// 8192 x 4096 bf16 30 -> 21 us.)
+// (P + 65535 - r) >> 16, one up when r < rint(p 2^16): byte 2 of the sum.  (By the exponent of a it takes four operations of the integer pipe, here one: rows
+// of 8192 x 4096 bf16 30 -> 27 us; with three scalar multiply-adds an element instead of half as many packed ones 1 us more.)
 __device__ __forceinline__ float min3(float a, float b, float c) { float r; asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // Byte 3 of four words.
 __device__ __forceinline__ uint32_t byte3_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {

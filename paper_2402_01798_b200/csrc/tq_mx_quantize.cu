@@ -162,6 +162,7 @@ __device__ __forceinline__ int within(uint64_t size, uint64_t from, int most) {
     return from >= size ? 0 : size - from < static_cast<uint64_t>(most) ? static_cast<int>(size - from) : most;
 }
 
+// 8192 x 4096 bf16 along both axes: nearest 23.5 us (4.4 TB/s), stochastic 44, the integer and fma-heavy pipes 60 % busy each with 32 instructions an element.
 template <bool BF16, bool STOCHASTIC, bool BOTH>
 __global__ void __launch_bounds__(kThreads, 4) mx_tile_kernel(MxInput in, MxView out, MxView out_t, uint32_t tiles_across, RoundKeys keys, uint32_t first_row) {
     extern __shared__ __align__(16) unsigned char raw[];
@@ -234,7 +235,8 @@ __device__ __forceinline__ uint64_t mx_scale_row(const MxView& m, uint32_t row) 
     return m.tiles ? (row >> 7) * m.scale_stride + (row & 31) * 16 + ((row >> 5) & 3) * 4 : row * m.scale_stride;
 }
 
-// Rows that start on 16-byte boundaries (`wide`: 32): 16 elements of 2 rows, stored in pieces of 32 or 16 bytes.
+// Rows that start on 16-byte boundaries (`wide`: 32): 16 elements of 2 rows, stored in pieces of 32 or 16 bytes.  8192 x 4096 to bf16: 11.8 us, 7.2 TB/s of the L2
+// and memory (with 8 elements of 4 rows, more of it addresses, 15).
 constexpr int kWideEach = 16, kWideRows = 2;
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxView m, void* out, uint64_t stride, uint32_t chunks, uint32_t shift, uint32_t wide) {
@@ -298,7 +300,8 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(MxView m, void*
 }
 
 // Rows on any boundary: 8 elements of 4 rows; a warp's 256 go through shared memory, so that consecutive threads store consecutive words.  bf16 rows may
-// start in the middle of a word: two elements a thread all the same, the first and last alone.
+// start in the middle of a word: two elements a thread all the same, the first and last alone.  8191 x 5003: to fp32 32 us (5.8 TB/s), to bf16 27 (3.9 TB/s), bound by
+// instructions, some 19 an element.  (Two words of codes shifted to the output's own 16-byte pieces, without shared memory: 39 and 31 us.)
 constexpr int kRaggedEach = 8, kRaggedRows = 4;
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_ragged_kernel(MxView m, void* out, uint64_t stride, uint32_t chunks, uint32_t shift) {
@@ -334,30 +337,40 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_ragged_kernel(MxView m
         for (int e = 0; e < 8; e += 2) unpair(mul2(pair(v[e], v[e + 1]), scale), v[e], v[e + 1]);
         __syncwarp();
         if constexpr (BF16) {
-            *reinterpret_cast<uint4*>(&words[4 * lane]) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-            __syncwarp();
             unsigned short* const to = static_cast<unsigned short*>(out) + row * stride + first;
-            const int off = static_cast<int>(reinterpret_cast<uintptr_t>(to) >> 1 & 1);
+            const int off = static_cast<int>(reinterpret_cast<uintptr_t>(to) >> 1 & 1);      // 1: the row starts in the middle of a word, and words hold elements 2t - 1 and 2t
+            const float before = __shfl_up_sync(0xFFFFFFFFu, v[7], 1);
+            *reinterpret_cast<uint4*>(&words[4 * lane]) = off ? make_uint4(pack_bf16(before, v[0]), pack_bf16(v[1], v[2]), pack_bf16(v[3], v[4]), pack_bf16(v[5], v[6]))
+                                                              : make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            __syncwarp();
+            unsigned short* const mine = to + 2 * static_cast<int>(lane) - off;
+            if (off && lane == 31 && count == 256) to[255] = static_cast<unsigned short>(__float_as_uint(v[7]) >> 16);
+            if (count == 256 && !(off && lane == 0)) {
 #pragma unroll
-            for (int k = 0; k < 5; ++k) {
-                const int t = 32 * k + static_cast<int>(lane), e = 2 * t - off;          // elements e and e + 1
-                if (k == 4 && (lane != 0 || off == 0)) break;
-                const uint32_t here = t < 128 ? words[t] : 0u, before = off && t > 0 ? words[t - 1] : 0u;
-                const uint32_t two = off ? __byte_perm(before, here, 0x5432) : here;
-                if (e >= 0 && e + 1 < count) asm volatile("st.global.b32 [%0], %1;" ::"l"(to + e), "r"(two) : "memory");
-                else if (e >= 0 && e < count) to[e] = static_cast<unsigned short>(two);
-                else if (e == -1 && count > 0) to[0] = static_cast<unsigned short>(two >> 16);
+                for (int k = 0; k < 4; ++k) asm volatile("st.global.b32 [%0], %1;" ::"l"(mine + 64 * k), "r"(words[32 * k + lane]) : "memory");
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int e = 2 * (32 * k + static_cast<int>(lane)) - off;
+                    const uint32_t two = words[32 * k + lane];
+                    if (e >= 0 && e + 1 < count) asm volatile("st.global.b32 [%0], %1;" ::"l"(to + e), "r"(two) : "memory");
+                    else if (e >= 0 && e < count) to[e] = static_cast<unsigned short>(two);
+                    else if (e == -1) to[0] = static_cast<unsigned short>(two >> 16);
+                }
             }
         } else {
 #pragma unroll
             for (int q = 0; q < 2; ++q)
                 *reinterpret_cast<float4*>(&words[8 * lane + 4 * q]) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
             __syncwarp();
-            float* const to = static_cast<float*>(out) + row * stride + first;
+            float* const to = static_cast<float*>(out) + row * stride + first + lane;
+            if (count == 256) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int e = 32 * k + static_cast<int>(lane);
-                if (e < count) to[e] = __uint_as_float(words[e]);
+                for (int k = 0; k < 8; ++k) to[32 * k] = __uint_as_float(words[32 * k + lane]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (32 * k + static_cast<int>(lane) < count) to[32 * k] = __uint_as_float(words[32 * k + lane]);
             }
         }
     }
@@ -391,7 +404,8 @@ __device__ __forceinline__ void divide8(float (&v)[8], float n, float inv, bool 
     }
 }
 // A thread decodes the same EACH elements of every worker's row (32, a block; 8 where the rows are too short to fill the GPU so) and keeps their sums.
-// fp32, in worker order; code * scale is exact, so that one fused operation adds it.
+// fp32, in worker order; code * scale is exact, so that one fused operation adds it.  16 x 25.6 M: 63 us, 5.1 TB/s; four workers' codes are asked for at a time
+// (two 66 us, eight 69).
 template <bool WEIGHTED, int EACH>
 __global__ void __launch_bounds__(kThreads) mx_aggregate_kernel(MxView m, float* out, uint32_t n, float divisor, float inv, bool exact, MxWeights weights) {
     pdl_wait();
@@ -494,7 +508,8 @@ __device__ __forceinline__ void take_ahead(const MxAhead& a, int j, const MxItem
     }
 }
 
-// A block takes tile after tile.  AHEAD: as above, 102 KB of shared memory, two blocks an SM.
+// A block takes tile after tile.  AHEAD: as above, 102 KB of shared memory, two blocks an SM.  8192 x 8192 bf16: stochastic 250 us, 93 instructions a feature at 0.7 a
+// clock and scheduler; nearest 154 (3.8 TB/s).  Three blocks a tile, one for each of dg, du and h, with half the registers: 331.
 template <bool BF16, bool AHEAD, bool GELU, bool STOCHASTIC>
 __global__ void __launch_bounds__(kThreads, 2) mx_gated_backward_kernel(MxGatedInput in, MxView dgu, MxView dgu_t, MxView h_t, uint32_t tiles_across, uint32_t tiles, RoundKeys keys) {
     extern __shared__ __align__(16) unsigned char raw[];
