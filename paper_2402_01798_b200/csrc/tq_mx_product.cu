@@ -135,6 +135,7 @@ struct ProductArgs {
     uint64_t a_band, b0_band, b1_band;                           // bytes between 128 rows
     uint32_t m, n, k;                                            // n: columns of C, or features
     uint32_t tiles_m, tiles_n;
+    uint32_t group;                                              // of tiles in m (pair kernel)
     uint32_t a_rows;                                             // rows of A in a box
     void* out;                                                   // C, or the two projections (may be null)
     uint64_t out_stride;
@@ -245,6 +246,18 @@ constexpr uint32_t kPairSmem = kPairStages * kPairStage + 1024 + 256;
 constexpr uint32_t kSecond = 112, kPairScales = kSecond + 256, kPairScaleColumns = 24;
 static_assert(kPairScales + kPairStages * kPairScaleColumns == 512, "tensor memory has 512 columns");
 
+// Tile t of the result.  The tiles that are worked on at a time are a column of `group` tiles and as many to its right as there are clusters: where both operands fit
+// the L2 together the whole height is taken, else 4, so that a wave of tiles reads little of either (8192 x 4096 x 16384, 107 MB of operands: 202 us with the whole height,
+// 180 with 4, after a second of it 240 and 208; 8192^3, 71 MB: 188 and 192).
+struct PairTile {
+    uint32_t m, n;
+    __device__ __forceinline__ PairTile(const ProductArgs& p, uint32_t t) {
+        const uint32_t per = p.group * p.tiles_n, first = t / per * p.group, in = t % per, high = p.tiles_m - first < p.group ? p.tiles_m - first : p.group;
+        m = first + in % high;
+        n = in / high;
+    }
+};
+
 // GATED: 0 a plain product, 1 SiLU, 2 GELU.
 template <int GATED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0,
@@ -287,7 +300,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
         uint32_t it = 0;
         bool ok = true;
         for (uint32_t t = blockIdx.x / 2; t < tiles && ok; t += clusters) {
-            const uint32_t band = t % p.tiles_m * 2 + rank, n0 = t / p.tiles_m * kWide;
+            const PairTile tile(p, t);
+            const uint32_t band = tile.m * 2 + rank, n0 = tile.n * kWide;
             for (uint32_t c = 0; c < chunks; ++c, ++it) {
                 const int s = it % kPairStages;
                 if (!(ok = warp_wait(empty(s), ((it / kPairStages) & 1) ^ 1, &dead))) break;
@@ -358,7 +372,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
         const uint32_t tell = of_rank(drained, 0);
         uint32_t n_tile = 0;
         for (uint32_t t = blockIdx.x / 2; t < tiles; t += clusters, ++n_tile) {
-            const uint32_t band = t % p.tiles_m * 2 + rank, n0 = t / p.tiles_m * kWide;
+            const PairTile tile(p, t);
+            const uint32_t band = tile.m * 2 + rank, n0 = tile.n * kWide;
             if (!warp_wait(done, n_tile & 1, &dead)) break;
             fence_after();
             const uint32_t local = quarter * 32 + lane, row0 = band * 128 + quarter * 32;
@@ -1037,6 +1052,8 @@ cudaError_t launch_product_as(const tq_mx_t& a, const tq_mx_t& b0, const tq_mx_t
     }
     if (plan.pair) {
         p.tiles_m = (p.m + 255) / 256; p.tiles_n = (p.n + (GATED ? 127 : 255)) / (GATED ? 128 : 256);
+        const uint64_t operands = (static_cast<uint64_t>(p.m) + static_cast<uint64_t>(p.n) * (GATED ? 2 : 1)) * p.k * 17 / 32;
+        p.group = operands > 80'000'000 && p.tiles_m > 4 ? 4 : p.tiles_m;
         const uint32_t tiles = p.tiles_m * p.tiles_n, pairs = static_cast<uint32_t>(sm_count()) / 2;
         ScaleMaps maps;
         if (const cudaError_t e = scales_map(&maps.a, a)) return e;

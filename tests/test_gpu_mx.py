@@ -234,6 +234,20 @@ def test_few_rows_with_long_sums(tq, m):
         assert (np.abs(half.cpu().double().numpy() - want) <= bound + 2.0 ** -24 * (np.abs(want) + bound)).all()
 
 
+def test_product_with_operands_beyond_the_cache(tq):
+    """Tiles in groups of rows, the last group ragged: the rows of one call are those of calls on parts of it, which take the tiles in another order.  The parts
+    are tall enough for the same kernel, which adds k in one order whatever the tile's place."""
+    rng = np.random.default_rng(12)
+    a, b = random_mx(tq, rng, 5400, 16384, 1), random_mx(tq, rng, 5000, 16384, 1)
+    whole = tq.tq_mx_product(a, b, torch.float32)
+    assert (5400 + 5000) * 16384 * 17 // 32 > 80_000_000
+    for first, rows in ((0, 2560), (2560, 2840)):
+        part = tq.MxMatrix(a.codes[first:first + rows], a.scales[first // 128:], rows, 16384)
+        assert torch.equal(whole[first:first + rows], tq.tq_mx_product(part, b, torch.float32))
+    va, vb = values(a)[5300:], values(b)
+    assert (np.abs(whole[5300:].cpu().double().numpy() - va @ vb.T) <= sum_bound(va, vb, 16384) * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(va @ vb.T)).all()
+
+
 def test_product_scales_reach_the_ends(tq):
     """Every scale byte, and NaN blocks: a row of one operand that holds one is NaN, the others are untouched."""
     rng = np.random.default_rng(4)
