@@ -377,6 +377,9 @@ tq_status tq_decompress_aggregate_segments(const uint32_t* packed_dev, size_t wo
  *   tq_mx_code_stride(cols) and tq_mx_scale_stride(cols, layout).  A scale buffer has `rows` rows (TQ_MX_ROWS) or ceil(rows / 128)
  *   (TQ_MX_TILES).  Rows, and columns at multiples of 128, of a larger matrix make a matrix of their own (in TQ_MX_TILES rows from a multiple of 128).
  * rows < 2^31; cols <= 2^40 (below 2^31 in the products).
+ * These calls only enqueue work on `stream`, each one kernel; they use no scratch memory and keep nothing, so calls on different streams may overlap, and they can
+ * be captured into graphs (call each once outside a capture first: the first launch of a kernel sets a function attribute).
+ * A call writes exactly its outputs' elements, the zeros behind a row's last code in its block, and in TQ_MX_TILES the zeros that fill the last scale tiles.
  */
 typedef enum { TQ_MX_TILES = 0, TQ_MX_ROWS = 1 } tq_mx_layout;
 typedef enum {

@@ -54,7 +54,7 @@ __device__ __forceinline__ float mx_scale_value(uint32_t byte) {
     return __uint_as_float(byte == 255u ? 0x7FC00000u : byte == 0u ? 0x00400000u : byte << 23);
 }
 
-// Two scaled elements -> two codes in the low byte, to nearest, ties to even, 6 at most.
+// Eight scaled elements -> eight codes, to nearest, ties to the even code, 6 at most; the sign of a zero stays.
 __device__ __forceinline__ uint32_t e2m1_nearest8(const float (&v)[8]) {
     uint32_t r;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
