@@ -484,7 +484,9 @@ def _is_bf16(dtype: torch.dtype) -> bool:
 
 def tq_mx_quantize(x: torch.Tensor, rounding: int = MX_NEAREST, seed: int = 0, first_row: int = 0, cols: Optional[int] = None,
                    layout: int = MX_TILES, out: Optional[MxMatrix] = None, stream=None) -> MxMatrix:
-    """Enqueue the quantisation of ``x`` ([rows, cols] or [cols], fp32 or bf16) along its rows; the first ``cols`` columns when given."""
+    """Enqueue the quantisation of ``x`` ([rows, cols] or [cols], fp32 or bf16) along its rows; the first ``cols`` columns when given.
+
+    As in all calls on matrices, tensors and ``out`` have the sizes of the call; of larger ones the part that is meant is passed."""
     return _made(_calls().mx_quantize(x, rounding, seed, first_row, cols, layout, out, stream), "tq_mx_quantize")
 
 
@@ -500,7 +502,8 @@ def tq_mx_dequantize(m: MxMatrix, dtype: torch.dtype = torch.float32, out: Optio
 
 
 def tq_mx_decompress_aggregate(m: MxMatrix, weights: Optional[Sequence[float]] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """Enqueue the mean (or weighted sum) of the rows of ``m`` (layout MX_ROWS); returns the [cols] fp32 update."""
+    """Enqueue the mean (or weighted sum) of the rows of ``m`` (layout MX_ROWS); returns the [cols] fp32 update.  ``out`` may be longer: what lies
+    behind the columns stays."""
     return _made(_calls().mx_decompress_aggregate(m, weights, out, stream), "tq_mx_decompress_aggregate")
 
 

@@ -453,13 +453,15 @@ tq_mx_t mx(PyObject* o) {
     m.scales = bytes_of(o, N.own_scales, "scales", tiles ? m.rows / 128 + (m.rows % 128 != 0) : m.rows, tiles ? (blocks + 3) / 4 * 512 : (blocks + 15) / 16 * 16, &m.scale_stride);
     return m;
 }
-// A plain [rows, cols] tensor, fp32 or bf16; a vector is one row.  At least `rows` x `cols` where those are given.
+// A plain [rows, cols] tensor, fp32 or bf16; a vector is one row.
 struct Plain {
     void* data;
     tq_dtype dtype;
     uint64_t stride;
 };
-Plain plain(const at::Tensor& t, const char* what, uint64_t rows, uint64_t cols) {
+// Its size is that of the call: of a larger tensor the part that is meant has to be passed, or projections of more features would give u from
+// g's columns.  `longer`: rows may have more elements than the call takes.
+Plain plain(const at::Tensor& t, const char* what, uint64_t rows, uint64_t cols, bool longer = false) {
     on_current_device(t, what);
     const int64_t dims = t.dim();
     if ((dims != 1 && dims != 2) || (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1)) fail(PyExc_ValueError, (std::string(what) + " must be [rows, cols] with unit inner stride").c_str());
@@ -469,6 +471,7 @@ Plain plain(const at::Tensor& t, const char* what, uint64_t rows, uint64_t cols)
     else fail(PyExc_TypeError, (std::string(what) + " must be float32 or bfloat16").c_str());
     const uint64_t have = dims == 2 ? static_cast<uint64_t>(t.size(0)) : 1u, wide = static_cast<uint64_t>(t.size(dims - 1));
     if (have < rows || wide < cols) fail(PyExc_ValueError, (std::string(what) + " is smaller than the call needs").c_str());
+    if (have > rows || (wide > cols && !longer)) fail(PyExc_ValueError, (std::string(what) + " is larger than the call needs").c_str());
     if (have > 1 && rows > 1 && t.stride(0) < static_cast<int64_t>(cols)) fail(PyExc_ValueError, (std::string(what) + " has rows that overlap").c_str());
     p.data = t.data_ptr();
     p.stride = have > 1 ? static_cast<uint64_t>(t.stride(0)) : wide;
@@ -588,7 +591,8 @@ PyObject* mx_quantize(Args& a) {                // x, rounding, seed, first_row,
     if (PyErr_Occurred()) throw Failed();
     Owned out = matrix_or_new(a, x, high(x), cols, layout);
     const tq_mx_t m = mx(out.get());
-    const Plain p = plain(x, "x", m.rows, m.cols);
+    if (m.cols != cols) fail(PyExc_ValueError, m.cols < cols ? "out has fewer columns than are quantised" : "out has more columns than are quantised");
+    const Plain p = plain(x, "x", m.rows, m.cols, c != Py_None);
     return made(call(F.mx_quantize, p.data, p.dtype, p.stride, static_cast<tq_mx_rounding>(rounding), seed, first, &m, a.stream()), out);
 }
 PyObject* mx_quantize_both(Args& a) {           // x, rounding, seed, first_row, out, out_t, stream
@@ -616,7 +620,7 @@ PyObject* mx_decompress_aggregate(Args& a) {    // matrix, weights, out, stream
     const tq_mx_t m = mx(o);
     const float* w = a.weights(static_cast<uint32_t>(m.rows < TQ_MAX_WORKERS ? m.rows : TQ_MAX_WORKERS));
     Owned out = tensor_or_new(a, tensor_of(o), -1, static_cast<int64_t>(m.cols), false);
-    const Plain p = plain(THPVariable_Unpack(out.get()), "out", 1, m.cols);
+    const Plain p = plain(THPVariable_Unpack(out.get()), "out", 1, m.cols, true);
     if (p.dtype != TQ_F32) fail(PyExc_TypeError, "out must be float32");
     return made(call(F.mx_decompress_aggregate, &m, w, static_cast<float*>(p.data), a.stream()), out);
 }
