@@ -444,7 +444,10 @@ tq_status tq_mx_product(const tq_mx_t* a_host, const tq_mx_t* b_host, void* out_
  * The first half of a gated feed-forward block: with g = x w_gate^T and u = x w_up^T,
  *     h = quantised (nearest, along the rows) act(g) * u.
  * x [tokens][d], w_gate and w_up [features][d], h [tokens][features], all TQ_MX_TILES; features a multiple of 32, d >= 1.  g and u
- * stay on the chip in fp32; h is made from them without an intermediate rounding.
+ * stay on the chip in fp32; h is made from them without an intermediate rounding to a smaller type.
+ * act(x) = x sigmoid(z), with z = x or 2 sqrt(2/pi) (x + 0.044715 x^3), is off by less than 2^-20 of itself, for GELU 2^-21 |z| of itself more,
+ * wherever it is a normal fp32 number, and gradual underflow follows; act'(x) = sigmoid(z) + x z' sigmoid(z) sigmoid(-z) by less than
+ * 2^-19 (GELU: 2^-20 |z| more) of the sum of its terms' magnitudes.
  *   projections_dev  NULL, or where the training step keeps [g | u] for tq_mx_gated_backward: [tokens][2 features] of `dtype`, proj_stride
  *                    elements from row to row.
  * Errors as for tq_mx_product.
