@@ -2,7 +2,8 @@
 
 Only argument marshalling happens here and, for the calls of a round, in the compiled module ``_tq_python``
 (csrc/tq_python.cpp).  Tensors are torch tensors used as typed device buffers; the stream is torch's current
-CUDA stream unless one is given.
+CUDA stream unless one is given.  Tensors that a call makes for a given stream are that stream's memory; the caller orders
+it and the current stream, before the call for the inputs and before the results are used.
 """
 from __future__ import annotations
 
@@ -173,6 +174,26 @@ def _calls():
     return _native
 
 
+def _empty(size, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """Memory for what a call makes or needs while it runs.  With a stream other than the current one it is that stream's memory: work before on the
+    current stream may still use what its memory last held, and what a call drops could be handed out again while its kernels run.  The current stream
+    is noted, so that results may be used and dropped there once the caller has ordered the two."""
+    if stream is None:
+        return torch.empty(size, dtype=dtype, device=device)
+    device = torch.device(device)
+    if device.type != "cuda":
+        return torch.empty(size, dtype=dtype, device=device)
+    if device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    handle, current = int(getattr(stream, "cuda_stream", stream)), torch.cuda.current_stream(device)
+    if handle == current.cuda_stream:
+        return torch.empty(size, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)):
+        t = torch.empty(size, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
 def _check(status: int, where: str) -> None:
     if status != OK:
         L = lib()
@@ -209,9 +230,9 @@ def tq_stats(grad: torch.Tensor, d: Optional[int] = None, g_min: float = 0.0, ka
              stats_dev: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """Enqueue the statistics reduction; returns the device tensor holding n_workers 64-byte records."""
     if stats_dev is None:
-        stats_dev = torch.empty(_rows(grad) * 64, dtype=torch.uint8, device=grad.device)
+        stats_dev = _empty(_rows(grad) * 64, torch.uint8, grad.device, stream)
     if workspace is None:
-        workspace = torch.empty(tq_stats_workspace_bytes(_rows(grad)), dtype=torch.uint8, device=grad.device)
+        workspace = _empty(tq_stats_workspace_bytes(_rows(grad)), torch.uint8, grad.device, stream)
     _check(_calls().stats(grad, d, g_min, kappa, stats_dev, workspace, stream), "tq_stats")
     return stats_dev
 
@@ -224,9 +245,9 @@ def tq_stats_hinted(grad: torch.Tensor, hint: torch.Tensor, d: Optional[int] = N
     round to round; zero it before the first one (``new_gmin_hint``).  Returns the records' device tensor.
     """
     if stats_dev is None:
-        stats_dev = torch.empty(_rows(grad) * 64, dtype=torch.uint8, device=grad.device)
+        stats_dev = _empty(_rows(grad) * 64, torch.uint8, grad.device, stream)
     if workspace is None:
-        workspace = torch.empty(tq_stats_workspace_bytes(_rows(grad)), dtype=torch.uint8, device=grad.device)
+        workspace = _empty(tq_stats_workspace_bytes(_rows(grad)), torch.uint8, grad.device, stream)
     _check(_calls().stats_hinted(grad, d, kappa, hint, stats_dev, workspace, stream), "tq_stats_hinted")
     return stats_dev
 
@@ -293,8 +314,7 @@ def tq_compress(grad: torch.Tensor, params: Sequence[Params], seed: int, first_w
                 d: Optional[int] = None, packed: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue truncate + stochastic round + pack for all rows of ``grad``; returns [N, words] int32."""
     if packed is None:
-        packed = torch.empty((_rows(grad), tq_packed_words(grad.shape[-1] if d is None else d, params[0].bits)), dtype=torch.int32,
-                             device=grad.device)
+        packed = _empty((_rows(grad), tq_packed_words(grad.shape[-1] if d is None else d, params[0].bits)), torch.int32, grad.device, stream)
     _check(_calls().compress(grad, d, _params_array(params), seed & 0xFFFFFFFFFFFFFFFF, first_worker, packed, stream), "tq_compress")
     return packed
 
@@ -304,7 +324,7 @@ def tq_decompress_aggregate(packed: torch.Tensor, d: int, params: Sequence[Param
                             stream=None) -> torch.Tensor:
     """Enqueue unpack + dequantize + average of the N packed rows; returns the [d] fp32 update."""
     if out is None:
-        out = torch.empty(d, dtype=torch.float32, device=packed.device)
+        out = _empty(d, torch.float32, packed.device, stream)
     _check(_calls().decompress_aggregate(packed, d, _params_array(params), weights, out, stream), "tq_decompress_aggregate")
     return out
 
@@ -317,7 +337,7 @@ def tq_decompress_aggregate_rows(rows: Sequence, d: int, params: Sequence[Params
     alive until the stream has passed the call."""
     if out is None:
         dev = next((r.device for r in rows if not isinstance(r, int)), "cuda")
-        out = torch.empty(d, dtype=torch.float32, device=dev)
+        out = _empty(d, torch.float32, dev, stream)
     _check(_calls().decompress_aggregate_rows(rows, d, _params_array(params), weights, out, stream), "tq_decompress_aggregate_rows")
     return out
 
@@ -327,7 +347,7 @@ def tq_params_device(stats_dev: torch.Tensor, n_workers: int, num_levels: int, m
                      params_dev: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue the parameter design on the device; returns the device tensor of n_workers 176-byte records."""
     if params_dev is None:
-        params_dev = torch.empty(n_workers * C.sizeof(Params), dtype=torch.uint8, device=stats_dev.device)
+        params_dev = _empty(n_workers * C.sizeof(Params), torch.uint8, stats_dev.device, stream)
     _check(_calls().params_device(stats_dev, n_workers, num_levels, mode, gamma, alpha_rule, alpha_user, params_dev, stream), "tq_params_device")
     return params_dev
 
@@ -343,7 +363,7 @@ def tq_compress_device_params(grad: torch.Tensor, params_dev: torch.Tensor, num_
                               first_worker: int = 0, d: Optional[int] = None, packed: Optional[torch.Tensor] = None,
                               stream=None) -> torch.Tensor:
     if packed is None:
-        packed = torch.empty((_rows(grad), tq_packed_words(grad.shape[-1] if d is None else d, _BITS[num_levels])), dtype=torch.int32, device=grad.device)
+        packed = _empty((_rows(grad), tq_packed_words(grad.shape[-1] if d is None else d, _BITS[num_levels])), torch.int32, grad.device, stream)
     _check(_calls().compress_device_params(grad, d, params_dev, num_levels, mode, seed & 0xFFFFFFFFFFFFFFFF, first_worker, packed, stream), "tq_compress_device_params")
     return packed
 
@@ -352,7 +372,7 @@ def tq_decompress_aggregate_device_params(packed: torch.Tensor, d: int, params_d
                                           weights: Optional[Sequence[float]] = None,
                                           out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     if out is None:
-        out = torch.empty(d, dtype=torch.float32, device=packed.device)
+        out = _empty(d, torch.float32, packed.device, stream)
     _check(_calls().decompress_aggregate_device_params(packed, d, params_dev, num_levels, weights, out, stream), "tq_decompress_aggregate_device_params")
     return out
 
@@ -373,9 +393,9 @@ def tq_stats_segments(grad: torch.Tensor, segments, g_min: float = 0.0, kappa: f
     """One record per (worker, segment), index worker * n_segments + segment; returns the device records."""
     seg = segments if isinstance(segments, C.Array) else segments_array(segments)
     if stats_dev is None:
-        stats_dev = torch.empty(_rows(grad) * len(seg) * C.sizeof(Stats), dtype=torch.uint8, device=grad.device)
+        stats_dev = _empty(_rows(grad) * len(seg) * C.sizeof(Stats), torch.uint8, grad.device, stream)
     if workspace is None:
-        workspace = torch.empty(tq_stats_workspace_bytes(_rows(grad) * len(seg)), dtype=torch.uint8, device=grad.device)
+        workspace = _empty(tq_stats_workspace_bytes(_rows(grad) * len(seg)), torch.uint8, grad.device, stream)
     _check(_calls().stats_segments(grad, seg, g_min, kappa, stats_dev, workspace, stream), "tq_stats_segments")
     return stats_dev
 
@@ -386,9 +406,9 @@ def tq_stats_hinted_segments(grad: torch.Tensor, segments, hint: torch.Tensor, k
     """tq_stats_hinted for every (worker, segment) pair; `hint` = new_gmin_hint(n_workers * n_segments), kept across rounds."""
     seg = segments if isinstance(segments, C.Array) else segments_array(segments)
     if stats_dev is None:
-        stats_dev = torch.empty(_rows(grad) * len(seg) * C.sizeof(Stats), dtype=torch.uint8, device=grad.device)
+        stats_dev = _empty(_rows(grad) * len(seg) * C.sizeof(Stats), torch.uint8, grad.device, stream)
     if workspace is None:
-        workspace = torch.empty(tq_stats_workspace_bytes(_rows(grad) * len(seg)), dtype=torch.uint8, device=grad.device)
+        workspace = _empty(tq_stats_workspace_bytes(_rows(grad) * len(seg)), torch.uint8, grad.device, stream)
     _check(_calls().stats_hinted_segments(grad, seg, kappa, hint, stats_dev, workspace, stream), "tq_stats_hinted_segments")
     return stats_dev
 
@@ -397,7 +417,7 @@ def tq_compress_segments(grad: torch.Tensor, segments, params_dev: torch.Tensor,
                          first_worker: int = 0, packed: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     seg = segments if isinstance(segments, C.Array) else segments_array(segments)
     if packed is None:
-        packed = torch.empty((_rows(grad), tq_segments_packed_words(seg, _BITS[num_levels])), dtype=torch.int32, device=grad.device)
+        packed = _empty((_rows(grad), tq_segments_packed_words(seg, _BITS[num_levels])), torch.int32, grad.device, stream)
     _check(_calls().compress_segments(grad, seg, params_dev, num_levels, mode, seed & 0xFFFFFFFFFFFFFFFF, first_worker, packed, stream), "tq_compress_segments")
     return packed
 

@@ -6,6 +6,8 @@
 
 #include <ATen/EmptyTensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -117,8 +119,13 @@ public:
     }
     float f32() { return static_cast<float>(f64()); }
     // None: torch's current stream; else a stream object, or a raw handle: anything that int() takes (other libraries' handles do)
-    void* stream() {
-        PyObject* o = next();
+    void* stream() { return stream_of(next()); }
+    // The stream argument of a call whose last it is: for what is made before its turn.
+    PyObject* last() {
+        if (n_ < 1) fail(PyExc_TypeError, "too few arguments");
+        return args_[n_ - 1];
+    }
+    static void* stream_of(PyObject* o) {
         if (o == Py_None) return c10::cuda::getCurrentCUDAStream().stream();
         PyObject* handle = PyObject_HasAttrString(o, "cuda_stream") ? PyObject_GetAttrString(o, "cuda_stream") : PyNumber_Long(o);
         if (!handle) throw Failed();
@@ -479,10 +486,19 @@ Plain plain(const at::Tensor& t, const char* what, uint64_t rows, uint64_t cols,
 }
 // Memory from torch's allocator, as torch.empty takes it but straight: through the dispatcher a matrix costs 1.9 us of host time.  On the current device, where
 // the kernels run; a tensor for another one comes from at::empty.
-at::Tensor empty_like_device(const at::Tensor& like, at::IntArrayRef sizes, at::ScalarType type) {
-    if (like.is_cuda() && like.device().index() == c10::cuda::current_device())
-        return at::detail::empty_generic(sizes, c10::GetAllocator(c10::kCUDA), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
-    return at::empty(sizes, at::TensorOptions().dtype(type).device(like.device()));
+// It is the memory of `stream`, on which the call writes it: earlier work on the current stream may still use what that one's memory last held.  The
+// current stream, whose program drops the result, is noted for the allocator, which hands the memory out again when both have passed that.
+at::Tensor empty_like_device(const at::Tensor& like, at::IntArrayRef sizes, at::ScalarType type, PyObject* stream) {
+    if (!like.is_cuda() || like.device().index() != c10::cuda::current_device()) return at::empty(sizes, at::TensorOptions().dtype(type).device(like.device()));
+    const auto make = [&] { return at::detail::empty_generic(sizes, c10::GetAllocator(c10::kCUDA), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt); };
+    if (stream == Py_None) return make();
+    const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream();
+    const cudaStream_t given = static_cast<cudaStream_t>(Args::stream_of(stream));
+    if (current.stream() == given) return make();
+    const c10::cuda::CUDAStreamGuard on(c10::cuda::getStreamFromExternal(given, like.device().index()));
+    at::Tensor t = make();
+    c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
+    return t;
 }
 // A Python object that this call owns until it hands it over.
 class Owned {
@@ -500,7 +516,7 @@ private:
 PyObject* mx_class = nullptr;                   // binding.MxMatrix
 
 // A matrix in memory of its own, on the device of a tensor.
-Owned new_matrix(const at::Tensor& like, uint64_t rows, uint64_t cols, uint64_t layout) {
+Owned new_matrix(const at::Tensor& like, uint64_t rows, uint64_t cols, uint64_t layout, PyObject* stream) {
     if (rows >= (1ull << 31) || cols > (1ull << 40)) fail(PyExc_ValueError, "a matrix of this size is not possible");
     const int64_t bytes = static_cast<int64_t>(mx_place(rows, cols, layout == TQ_MX_TILES).bytes);
     static PyObject* const nothing = PyTuple_New(0);
@@ -511,7 +527,7 @@ Owned new_matrix(const at::Tensor& like, uint64_t rows, uint64_t cols, uint64_t 
         const Owned v(value);
         if (!value || PyObject_SetAttr(m.get(), name, value) != 0) throw Failed();
     };
-    set(N.memory, THPVariable_Wrap(empty_like_device(like, at::IntArrayRef(&bytes, 1), at::kByte)));
+    set(N.memory, THPVariable_Wrap(empty_like_device(like, at::IntArrayRef(&bytes, 1), at::kByte, stream)));
     set(N.rows, PyLong_FromUnsignedLongLong(rows));
     set(N.cols, PyLong_FromUnsignedLongLong(cols));
     set(N.layout, PyLong_FromUnsignedLongLong(layout));
@@ -524,7 +540,7 @@ Owned new_matrix(const at::Tensor& like, uint64_t rows, uint64_t cols, uint64_t 
 // The next argument, or for None a new matrix.
 Owned matrix_or_new(Args& a, const at::Tensor& like, uint64_t rows, uint64_t cols, uint64_t layout) {
     PyObject* o = a.next();
-    if (o == Py_None) return new_matrix(like, rows, cols, layout);
+    if (o == Py_None) return new_matrix(like, rows, cols, layout, a.last());
     Py_INCREF(o);
     return Owned(o);
 }
@@ -537,7 +553,7 @@ Owned tensor_or_new(Args& a, const at::Tensor& like, int64_t rows, int64_t cols,
         return Owned(o);
     }
     const int64_t sizes[2] = {rows, cols};
-    Owned t(THPVariable_Wrap(empty_like_device(like, rows < 0 ? at::IntArrayRef(&cols, 1) : at::IntArrayRef(sizes, 2), bf16 ? at::kBFloat16 : at::kFloat)));
+    Owned t(THPVariable_Wrap(empty_like_device(like, rows < 0 ? at::IntArrayRef(&cols, 1) : at::IntArrayRef(sizes, 2), bf16 ? at::kBFloat16 : at::kFloat, a.last())));
     if (!t.get()) throw Failed();
     return t;
 }
@@ -573,7 +589,7 @@ PyObject* made(tq_status s, std::initializer_list<Owned*> all) {
 PyObject* new_mx(Args& a) {                     // like, rows, cols, layout
     const at::Tensor& like = a.tensor();
     const uint64_t rows = a.u64(), cols = a.u64(), layout = a.u64();
-    return new_matrix(like, rows, cols, layout).release();
+    return new_matrix(like, rows, cols, layout, Py_None).release();
 }
 // Where a matrix in one piece is: (bytes of a row, row stride, first byte of the scales, their rows, their stride).
 PyObject* mx_layout(Args& a) {                  // rows, cols, layout

@@ -1,4 +1,4 @@
-"""Calls of the microscaled 4-bit operators as the binding takes them: sizes that do not fit, streams, memory that runs out."""
+"""Calls as the binding takes them: sizes that do not fit, and the memory of what a call makes for a given stream."""
 import pytest
 import torch
 
@@ -60,3 +60,130 @@ def test_parts_of_larger_tensors_are_taken(tq):
     out = torch.full((104,), -7.0, device="cuda")
     tq.tq_mx_decompress_aggregate(rows, out=out)
     assert torch.equal(out[:96], tq.tq_mx_decompress_aggregate(rows)) and (out[96:] == -7).all()
+
+
+# ---- a stream given by hand: what the call makes is that stream's memory -------------------------------------------------
+def pool_of(t):
+    """The stream whose memory a tensor lies in."""
+    for segment in torch.cuda.memory_snapshot():
+        if segment["address"] <= t.data_ptr() < segment["address"] + segment["total_size"]:
+            return segment["stream"]
+    raise AssertionError("not in the allocator's memory")
+
+
+def calls(tq):
+    """Every call that makes its outputs, as a function of the stream; the inputs are ready."""
+    g = torch.randn(3, 4096, device="cuda") * 1e-3
+    stats = tq.tq_stats(g)
+    params = [tq.tq_params(s, 16, tq.NONUNIFORM, gamma=3.0) for s in tq.stats_to_host(stats)]
+    params_dev = tq.tq_params_device(stats, 3, 16, tq.NONUNIFORM, 3.0)
+    packed = tq.tq_compress(g, params, seed=1)
+    groups = [(0, 1024), (1024, 2000)]
+    group_params = tq.tq_params_device(tq.tq_stats_segments(g, groups), 6, 16, tq.NONUNIFORM, 3.0)
+    x, m = torch.randn(64, 96, device="cuda"), tq.tq_mx_quantize(torch.randn(64, 96, device="cuda"))
+    rows, gu = tq.tq_mx_quantize(g, layout=tq.MX_ROWS), torch.randn(64, 192, device="cuda")
+
+    def hint(n):
+        h = tq.new_gmin_hint(n)
+        torch.cuda.synchronize()
+        return h
+    torch.cuda.synchronize()
+    return dict(
+        stats=lambda s: tq.tq_stats(g, stream=s),
+        stats_hinted=lambda s: tq.tq_stats_hinted(g, hint(3), stream=s),
+        stats_segments=lambda s: tq.tq_stats_segments(g, groups, stream=s),
+        stats_hinted_segments=lambda s: tq.tq_stats_hinted_segments(g, groups, hint(6), stream=s),
+        params_device=lambda s: tq.tq_params_device(stats, 3, 16, tq.NONUNIFORM, 3.0, stream=s),
+        compress=lambda s: tq.tq_compress(g, params, seed=1, stream=s),
+        compress_device_params=lambda s: tq.tq_compress_device_params(g, params_dev, 16, tq.NONUNIFORM, 1, stream=s),
+        compress_segments=lambda s: tq.tq_compress_segments(g, groups, group_params, 16, tq.NONUNIFORM, 1, stream=s),
+        aggregate=lambda s: tq.tq_decompress_aggregate(packed, 4096, params, stream=s),
+        aggregate_rows=lambda s: tq.tq_decompress_aggregate_rows(list(packed), 4096, params, stream=s),
+        aggregate_device_params=lambda s: tq.tq_decompress_aggregate_device_params(packed, 4096, params_dev, 16, stream=s),
+        mx_quantize=lambda s: tq.tq_mx_quantize(x, stream=s),
+        mx_quantize_both=lambda s: tq.tq_mx_quantize_both(x, stream=s),
+        mx_dequantize=lambda s: tq.tq_mx_dequantize(m, stream=s),
+        mx_decompress_aggregate=lambda s: tq.tq_mx_decompress_aggregate(rows, stream=s),
+        mx_product=lambda s: tq.tq_mx_product(m, m, stream=s),
+        mx_gated=lambda s: tq.tq_mx_gated(m, m, m, stream=s),
+        mx_gated_backward=lambda s: tq.tq_mx_gated_backward(x, gu, stream=s),
+    )
+
+
+def tensors(result):
+    return [t.memory if hasattr(t, "memory") else t for t in (result if isinstance(result, tuple) else (result,))]
+
+
+def test_results_are_memory_of_the_given_stream(tq):
+    for name, call in calls(tq).items():
+        stream = torch.cuda.Stream()
+        want = [t.clone() for t in tensors(call(None))]
+        torch.cuda.synchronize()
+        for given in (stream, stream.cuda_stream):                     # an object, a handle
+            got = tensors(call(given))
+            torch.cuda.synchronize()
+            for t, w in zip(got, want, strict=True):
+                assert pool_of(t) == stream.cuda_stream, name
+                if not name.startswith("mx"):                          # what lies between a matrix's rows is not written
+                    assert torch.equal(t, w), name
+        current = torch.cuda.current_stream()
+        for given in (None, current, current.cuda_stream):
+            got = tensors(call(given))
+            torch.cuda.synchronize()
+            assert all(pool_of(t) == current.cuda_stream for t in got), name
+
+
+def test_memory_in_use_on_the_current_stream_is_left_alone(tq):
+    """A block that the current stream frees while a slow kernel there has yet to read it: a call on another stream takes none of it."""
+    m = tq.tq_mx_quantize(torch.randn(1024, 1024, device="cuda"))
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        a = torch.full((1024, 1024), 7.0, device="cuda")
+        into = torch.zeros_like(a)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)                                  # some 10 ms
+        into.copy_(a)
+        del a
+        out = tq.tq_mx_dequantize(m, stream=stream)
+        torch.cuda.synchronize()
+        assert (into == 7).all()
+        del out
+
+
+def test_results_dropped_on_the_current_stream(tq):
+    """Used there after the given stream, and dropped while that use is still to come: the given stream's next call takes other memory."""
+    m = tq.tq_mx_quantize(torch.randn(1024, 1024, device="cuda"))
+    want = tq.tq_mx_dequantize(m)
+    other = tq.tq_mx_quantize(torch.zeros(1024, 1024, device="cuda"))
+    into, stream = torch.empty_like(want), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out = tq.tq_mx_dequantize(m, stream=stream)
+    torch.cuda.current_stream().wait_stream(stream)
+    torch.cuda._sleep(20_000_000)
+    into.copy_(out)
+    at = out.data_ptr()
+    del out
+    again = tq.tq_mx_dequantize(other, stream=stream)
+    assert again.data_ptr() != at
+    torch.cuda.synchronize()
+    assert torch.equal(into, want)
+
+
+def test_streams_by_hand_inside_a_graph(tq):
+    """A call on a forked stream of a capture makes its outputs in the graph's memory."""
+    m = tq.tq_mx_quantize(torch.randn(64, 96, device="cuda"))
+    want = tq.tq_mx_product(m, m)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = tq.tq_mx_product(m, m, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        twice = out + out
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(twice, want + want)
