@@ -15,7 +15,7 @@ NATIVE_SOURCE = os.path.join(CSRC, "tq_python.cpp")
 NATIVE_TORCH = os.path.join(PKG, "_tq_python.torch")       # the torch version that the module was built against: its C++ interface changes
 SOURCES = ["tq_api.cu", "tq_stats.cu", "tq_compress.cu", "tq_compress_lut.cu", "tq_decompress.cu", "tq_params.cu",
            "tq_mx_quantize.cu", "tq_mx_product.cu"]
-HEADERS = ["tq_aggregation_plan.h", "tq_device.cuh", "tq_launch.h", "tq_lut.cuh", "tq_mx.cuh"]
+HEADERS = ["tq_aggregation_plan.h", "tq_device.cuh", "tq_launch.h", "tq_lut.cuh", "tq_mx.cuh", "tq_wait.h"]
 
 NVCC_FLAGS = [
     "-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",

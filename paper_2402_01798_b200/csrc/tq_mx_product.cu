@@ -4,6 +4,7 @@
 #include <cuda.h>
 
 #include "tq_mx.cuh"
+#include "tq_wait.h"
 
 namespace tq {
 
@@ -107,21 +108,26 @@ __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
 }
 __device__ unsigned int g_product_wait_expired = 0;       // blocks whose bounded wait ran out, since load
 
-// A bounded wait that also ends when another thread of the block has given up.
-__device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, volatile int* dead) {
-    for (uint32_t it = 0; it < kWaitLimit; ++it) {
-        uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return true;
-        if ((it & 255u) == 255u && *dead) return false;
-    }
-    *dead = 1;
-    return false;
+// A bounded wait that also ends when another thread of the block has given up.  `filled`: stages that the block has asked for so far.  The wait for a sum
+// is renewed by them, the waits for a stage hardly ever see more than one.
+__device__ __forceinline__ bool wait_or_dead(uint32_t bar, uint32_t parity, volatile int* dead, volatile uint32_t* filled) {
+    const bool done = wait_with_progress(
+        kWaitLimit,
+        [&] {
+            uint32_t done;
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+            return done != 0;
+        },
+        [&] { return *dead != 0; }, [&] { return *filled; });
+    if (!done) *dead = 1;
+    return done;
 }
 
 // The same for all threads of a warp, with one answer.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* dead) { return __all_sync(0xFFFFFFFFu, wait_or_dead(bar, parity, dead)); }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* dead, volatile uint32_t* filled) {
+    return __all_sync(0xFFFFFFFFu, wait_or_dead(bar, parity, dead, filled));
+}
 // One thread of the warp issues.  The others go through the same loops, so that descriptors, addresses and barriers stay uniform over the warp: computed
 // by the one thread alone, they are moved to uniform registers one by one for each instruction, and a multiplication took 223 clocks where 128 are needed.
 __device__ __forceinline__ bool elect() {
@@ -265,6 +271,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
                                                                                           const __grid_constant__ ProductArgs p) {
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
+    __shared__ volatile uint32_t filled;
     __shared__ uint32_t tmem_base;
     __shared__ float scratch[8][kScratchWords];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
@@ -276,6 +283,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         dead = 0;
+        filled = 0;
         for (int s = 0; s < kPairStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1); mbar_init(drained, 16); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -304,7 +312,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
             const uint32_t band = tile.m * 2 + rank, n0 = tile.n * kWide;
             for (uint32_t c = 0; c < chunks; ++c, ++it) {
                 const int s = it % kPairStages;
-                if (!(ok = warp_wait(empty(s), ((it / kPairStages) & 1) ^ 1, &dead))) break;
+                if (!(ok = warp_wait(empty(s), ((it / kPairStages) & 1) ^ 1, &dead, &filled))) break;
                 if (leader) {
                     const uint32_t at = base + s * kPairStage, scales = at + kPairCodes, bar = of_rank(full(s), 0);
                     if (rank == 0) mbar_expect_tx(full(s), 2 * kPairStage);       // what lies outside the matrices arrives as zeros
@@ -313,6 +321,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
                     tma_load_pair(scales, &maps.a, c * 256, band, bar);
                     tma_load_pair(scales + 1024, &maps.b0, c * 256, n0 / 128, bar);
                     tma_load_pair(scales + 2048, GATED ? &maps.b1 : &maps.b0, c * 256, GATED ? n0 / 128 : n0 / 128 + 1, bar);
+                    filled = it + 1;
                 }
                 __syncwarp();
             }
@@ -334,19 +343,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
         };
         const uint32_t mine = (tiles - blockIdx.x / 2 + clusters - 1) / clusters, total = mine * chunks;
         const uint32_t last_steps = (p.k - (chunks - 1) * kBK + 63) / 64;
-        bool ok = warp_wait(full(0), 0, &dead);
+        bool ok = warp_wait(full(0), 0, &dead, &filled);
         if (ok) {
             fence_after();
             if (leader) copy_stage(0);
             __syncwarp();
         }
         for (uint32_t n_tile = 0, it = 0; n_tile < mine && ok; ++n_tile) {
-            if (!(ok = warp_wait(drained, (n_tile & 1) ^ 1, &dead))) break;
+            if (!(ok = warp_wait(drained, (n_tile & 1) ^ 1, &dead, &filled))) break;
             const uint32_t d = tmem + (n_tile & 1) * kSecond;
             for (uint32_t c = 0; c < chunks; ++c, ++it) {
                 const uint32_t s = it % kPairStages, next = (it + 1) % kPairStages;
                 const bool more = it + 1 < total;
-                if (more && !(ok = warp_wait(full(next), ((it + 1) / kPairStages) & 1, &dead))) break;
+                if (more && !(ok = warp_wait(full(next), ((it + 1) / kPairStages) & 1, &dead, &filled))) break;
                 fence_after();
                 if (leader) {
                     const uint64_t a = operand_desc(base + s * kPairStage), b = operand_desc(base + s * kPairStage + kPairCodes / 2);
@@ -374,7 +383,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
         for (uint32_t t = blockIdx.x / 2; t < tiles; t += clusters, ++n_tile) {
             const PairTile tile(p, t);
             const uint32_t band = tile.m * 2 + rank, n0 = tile.n * kWide;
-            if (!warp_wait(done, n_tile & 1, &dead)) break;
+            if (!warp_wait(done, n_tile & 1, &dead, &filled)) break;
             fence_after();
             const uint32_t local = quarter * 32 + lane, row0 = band * 128 + quarter * 32;
             const uint32_t from = tmem + (n_tile & 1) * kSecond + ((quarter * 32) << 16);
@@ -460,6 +469,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     using S = SplitShape<GATED>;
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
+    __shared__ volatile uint32_t filled;
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t barriers[2 * S::kStages + 2];
     __shared__ float scratch[8][kScratchWords];
@@ -471,6 +481,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         dead = 0;
+        filled = 0;
         for (uint32_t s = 0; s < stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -497,7 +508,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
         uint32_t s = 0, round = 0, it = 0;
         bool ok = true;
         for (uint32_t c = first; c < last; ++c, ++it) {
-            if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead))) break;
+            if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead, &filled))) break;
             if (leader) {
                 const uint32_t at = base + s * S::kStage, scales = at + at_scales;
                 const uint32_t bytes = (p.k + 127) / 128 - 2 * c < 2 ? 512 : 1024;
@@ -508,6 +519,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
                 bulk_load(scales, p.a_scales + tm * p.a_band + c * 1024ull, bytes, full(s));
                 bulk_load(scales + 1024, p.b0_scales + (n0 / 128) * p.b0_band + c * 1024ull, bytes, full(s));
                 if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024ull, bytes, full(s));
+                filled = it + 1;
             }
             __syncwarp();
             if (++s == stages) { s = 0; ++round; }
@@ -531,7 +543,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
         bool ok = true;
         uint32_t s = 0, round = 0;
         for (uint32_t c = first; c < last; ++c) {
-            if (!(ok = warp_wait(full(s), round & 1, &dead))) break;
+            if (!(ok = warp_wait(full(s), round & 1, &dead, &filled))) break;
             fence_after();
             if (leader) {
                 const uint32_t at = base + s * S::kStage;
@@ -564,7 +576,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     const bool taker = warp >= 2 && quarter * 32 < rows;        // has rows to take out of tensor memory
     bool fine = true;
     if (warp >= 2) {
-        fine = warp_wait(done, 0, &dead);
+        fine = warp_wait(done, 0, &dead, &filled);
         fence_after();
     }
     if constexpr (GATED != 0) {
@@ -721,6 +733,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
     constexpr int kSums = GATED ? 2 : 1;
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
+    __shared__ volatile uint32_t filled;
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t barriers[2 * S::kMostStages + 2];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
@@ -731,6 +744,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         dead = 0;
+        filled = 0;
         for (uint32_t s = 0; s < stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -756,7 +770,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
         uint32_t s = 0, round = 0, it = 0;
         bool ok = true;
         for (uint32_t c = first; c < last; ++c, ++it) {
-            if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead))) break;
+            if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead, &filled))) break;
             if (leader) {
                 const uint32_t at = base + s * stage_bytes, scales = at + at_scales;
                 const uint32_t bytes = (p.k + 127) / 128 - 2 * c < 2 ? 512 : 1024;
@@ -767,6 +781,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
                 if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024ull, bytes, full(s));
                 tma_load(at + S::kCodesB, &map_a, c * (kBK / 2), 0, full(s));
                 bulk_load(scales, p.a_scales + c * 1024ull, bytes, full(s));
+                filled = it + 1;
             }
             __syncwarp();
             if (++s == stages) { s = 0; ++round; }
@@ -780,7 +795,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
         uint32_t s = 0, round = 0;
         bool ok = true;
         for (uint32_t c = first; c < last; ++c) {
-            if (!(ok = warp_wait(full(s), round & 1, &dead))) break;
+            if (!(ok = warp_wait(full(s), round & 1, &dead, &filled))) break;
             fence_after();
             if (leader) {
                 const uint32_t at = base + s * stage_bytes, scales = at + at_scales;
@@ -817,7 +832,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
     const uint32_t from = tmem + ((quarter * 32) << 16);
     bool fine = true;
     if (warp >= 2) {
-        fine = warp_wait(done, 0, &dead);
+        fine = warp_wait(done, 0, &dead, &filled);
         fence_after();
     }
     if constexpr (GATED != 0) {

@@ -187,3 +187,19 @@ def test_streams_by_hand_inside_a_graph(tq):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(twice, want + want)
+
+
+def test_longest_sums(tq):
+    """Sums of close to 2^31 products: the wait for the whole of one lasts as long as its stages are filled.  All are ones, so that every partial sum is exact."""
+    k = 2 ** 31 - 256
+    ones_of = lambda rows, k: tq.MxMatrix(torch.full((rows, k // 2), 0x22, dtype=torch.uint8, device="cuda"),  # noqa: E731
+                                          torch.full((-(-rows // 128), k // 128 * 512), 127, dtype=torch.uint8, device="cuda"), rows, k)
+    a = ones_of(1, k)
+    assert tq.tq_mx_product(a, a, torch.float32).item() == k
+    assert tq.tq_wait_expired_count() == 0
+    del a
+    k = 2 ** 27 - 256
+    a, b = ones_of(130, k), ones_of(3, k)
+    assert (tq.tq_mx_product(a, b, torch.float32) == k).all()
+    del a, b
+    torch.cuda.empty_cache()
