@@ -481,8 +481,8 @@ uint64_t tq_kernel_launches(void); /* kernels launched by this library in this p
  * wait runs out there drops its own outputs and counts itself, so a tile can then be partly stored.
  * *count_host receives the number of such give-ups on the current device since the library was loaded
  * (0 in a healthy run: a non-zero value means the outputs of the affected launch are incomplete).  A block of a product gives up
- * when its wait has seen no stage of the sum asked for during that number of polls, so that long sums have their time.  It
- * stops there, counts itself once and leaves the rest of its outputs unwritten.
+ * when its wait has seen no stage of the sum asked for during that number of polls, so that long sums have their time.  It stops there, lets its copies and multiplications
+ * end, counts itself once and leaves the rest of its outputs unwritten, as do the blocks that add up the same outputs with it.
  * Synchronises the device.  Returns TQ_ERR_INVALID_ARG for a null pointer, TQ_ERR_CUDA if the read fails.
  * (The paper has no counterpart; this is a health check of the implementation.) */
 tq_status tq_wait_expired_count(uint32_t* count_host);

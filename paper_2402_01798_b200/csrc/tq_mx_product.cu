@@ -106,6 +106,14 @@ __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.a
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// A word of another block's shared memory, at the place of this block's `word`.
+__device__ __forceinline__ void tell_block(volatile uint32_t* word, uint32_t rank, uint32_t value) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(of_rank(smem_addr(const_cast<uint32_t*>(word)), rank)), "r"(value) : "memory");
+}
+// Bytes that are expected and will not come.
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 __device__ unsigned int g_product_wait_expired = 0;       // blocks whose bounded wait ran out, since load
 
 // A bounded wait that also ends when another thread of the block has given up.  `filled`: stages that the block has asked for so far.  The wait for a sum
@@ -271,7 +279,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
                                                                                           const __grid_constant__ ProductArgs p) {
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
-    __shared__ volatile uint32_t filled;
+    __shared__ volatile uint32_t filled, ended[2];                                   // ended: of either block, its fillings, and whether it gave up (bit 0)
     __shared__ uint32_t tmem_base;
     __shared__ float scratch[8][kScratchWords];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
@@ -302,10 +310,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
     const uint32_t tmem = tmem_base;
     const uint32_t tiles = p.tiles_m * p.tiles_n, chunks = (p.k + kBK - 1) / kBK, clusters = gridDim.x / 2;
     constexpr uint32_t kWide = GATED ? 128 : 256;                // columns of C, or features, in a tile
+    const bool leader = elect();
+    uint32_t issued = 0;                                         // warp 0: fillings of stages
 
     if (warp == 0) {
-        const bool leader = elect();
-        uint32_t it = 0;
+        uint32_t& it = issued;
         bool ok = true;
         for (uint32_t t = blockIdx.x / 2; t < tiles && ok; t += clusters) {
             const PairTile tile(p, t);
@@ -326,10 +335,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
                 __syncwarp();
             }
         }
-        if (!ok && rank == 0 && leader)                          // nothing may still be on its way into blocks that end
-            for (uint32_t j = it > kPairStages ? it - kPairStages : 0; j < it; ++j) mbar_wait(full(j % kPairStages), (j / kPairStages) & 1);
     } else if (warp == 1 && rank == 0) {
-        const bool leader = elect();
         // The scales of a stage are copied behind the multiplications of the stage before, so that a tile's first are in place when it begins
         // (8192 x 8192 x 512: 36.9 us, with copies in front of their own multiplications 38.6; no difference for long k).
         const auto copy_stage = [&](uint32_t s) {
@@ -371,10 +377,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
             }
             if (ok && leader) mma_commit<true>(done);
             __syncwarp();
-        }
-        if (!ok && leader) {                                     // let the multiplications that were issued come to an end
-            mma_commit<true>(flushed);
-            mbar_wait(flushed, 0);
         }
     } else if (warp >= 2) {
         const uint32_t quarter = warp % 4, half = (warp - 2) / 4;
@@ -427,7 +429,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) mx_
     }
     __syncwarp();
     __syncthreads();
+    if (warp == 0 && leader)
+        for (uint32_t r = 0; r < 2; ++r) tell_block(&ended[rank], r, issued << 1 | (dead != 0));
+    __syncwarp();
     cluster_sync();                                              // nobody leaves before the other's multiplications and messages are through
+    const uint32_t first_ended = ended[0], second_ended = ended[1];
+    if ((first_ended | second_ended) & 1) {                      // nor with anything on its way into either
+        if (warp == 0 && leader && rank == 0)
+            for_outstanding_of_pair(first_ended >> 1, second_ended >> 1, kPairStages, [&](uint32_t s, uint32_t parity, uint32_t by) {
+                if (by == 1) mbar_complete_tx(full(s), kPairStage);
+                if (by == 2) mbar_expect_tx(full(s), kPairStage);
+                mbar_wait(full(s), parity);
+            });
+        if (warp == 1 && leader) {
+            if (rank == 0) mma_commit<true>(flushed);
+            mbar_wait(flushed, 0);
+        }
+        __syncwarp();
+        cluster_sync();
+    }
     if (threadIdx.x == 0 && dead) atomicAdd(&g_product_wait_expired, 1u);
     fence_after();
     if (warp == 1) tmem_free<true>(tmem, 512);
@@ -469,7 +489,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     using S = SplitShape<GATED>;
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
-    __shared__ volatile uint32_t filled;
+    __shared__ volatile uint32_t filled, failed;                  // failed: a block of the cluster gave up
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t barriers[2 * S::kStages + 2];
     __shared__ float scratch[8][kScratchWords];
@@ -481,7 +501,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         dead = 0;
-        filled = 0;
+        filled = failed = 0;
         for (uint32_t s = 0; s < stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -502,13 +522,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     const uint32_t chunks = (p.k + kBK - 1) / kBK;
     const uint32_t first = chunks * rank / SPLIT, last = chunks * (rank + 1) / SPLIT;       // at least one: SPLIT <= chunks
     constexpr uint32_t at_a = S::kCodesB, at_scales = S::kCodesB + S::kCodesA;              // within a stage
+    const bool leader = elect();
+    uint32_t issued = 0;                                         // warp 0: fillings of stages
 
     if (warp == 0) {
-        const bool leader = elect();
-        uint32_t s = 0, round = 0, it = 0;
-        bool ok = true;
-        for (uint32_t c = first; c < last; ++c, ++it) {
-            if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead, &filled))) break;
+        uint32_t s = 0, round = 0;
+        for (uint32_t c = first; c < last; ++c, ++issued) {
+            if (!warp_wait(empty(s), (round & 1) ^ 1, &dead, &filled)) break;
             if (leader) {
                 const uint32_t at = base + s * S::kStage, scales = at + at_scales;
                 const uint32_t bytes = (p.k + 127) / 128 - 2 * c < 2 ? 512 : 1024;
@@ -519,16 +539,12 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
                 bulk_load(scales, p.a_scales + tm * p.a_band + c * 1024ull, bytes, full(s));
                 bulk_load(scales + 1024, p.b0_scales + (n0 / 128) * p.b0_band + c * 1024ull, bytes, full(s));
                 if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024ull, bytes, full(s));
-                filled = it + 1;
+                filled = issued + 1;
             }
             __syncwarp();
             if (++s == stages) { s = 0; ++round; }
         }
-        if (!ok && leader)                                       // nothing may still be on its way into a block that ends
-            for (uint32_t j = it > stages ? it - stages : 0; j < it; ++j) mbar_wait(full(j % stages), (j / stages) & 1);
-        __syncwarp();
     } else if (warp == 1) {
-        const bool leader = elect();
         const uint32_t n = GATED ? 256 : p.n - n0 < 128 ? (p.n - n0 + 15) / 16 * 16 : 128;
         const uint32_t last_steps = (p.k - (chunks - 1) * kBK + 63) / 64;
         const auto copy_stage = [&](uint32_t s) {                // of a chunk with one tile of scales the second is whatever lies there, and no step takes it
@@ -560,15 +576,19 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
             __syncwarp();
             if (++s == stages) { s = 0; ++round; }
         }
-        if (leader) {
-            if (ok) mma_commit<false>(done);
-            else {                                               // let the multiplications that were issued come to an end
-                mma_commit<false>(flushed);
-                mbar_wait(flushed, 0);
-            }
-        }
+        if (ok && leader) mma_commit<false>(done);
         __syncwarp();
     }
+    // Where a wait ran out: lets all that was issued end, before its memory is used again or the block leaves.
+    const auto settle = [&] {
+        if (dead == 0) return;
+        if (warp == 0 && leader) for_outstanding(issued, stages, [&](uint32_t s, uint32_t parity) { mbar_wait(full(s), parity); });
+        if (warp == 1 && leader) {
+            mma_commit<false>(flushed);
+            mbar_wait(flushed, 0);
+        }
+        __syncwarp();
+    };
     // Two warps for each quarter of the lanes.
     const uint32_t quarter = warp % 4, half = (warp - 2) / 4, local = quarter * 32 + lane, row0 = tm * 128 + quarter * 32;
     const uint32_t from = tmem + ((quarter * 32) << 16);
@@ -629,7 +649,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
             }
         };
         __syncthreads();
+        settle();
         cluster_sync();                                          // all blocks have multiplied: the stages are free
+        if (dead != 0 && threadIdx.x < SPLIT) tell_block(&failed, threadIdx.x, 1);
         if (taker && fine) {
 #pragma unroll 1
             for (uint32_t i = 0; i < SPLIT; ++i) {
@@ -641,7 +663,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
         }
         __syncthreads();
         cluster_sync();
-        if (taker && fine && half < Q::kHalves) {
+        if (taker && !failed && half < Q::kHalves) {
             const uint32_t col = n0 + rank * Q::kSlice + half * Q::kWidth;
             float v[Q::kWidth];
             const auto add_up = [&](float (&x)[Q::kWidth], uint32_t first_quad) {        // what the own block has in x with the others', in their order
@@ -675,6 +697,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
     __syncwarp();
     fence_before();
     __syncthreads();
+    if constexpr (SPLIT == 1) settle();
     if (threadIdx.x == 0 && dead) atomicAdd(&g_product_wait_expired, 1u);
     fence_after();
     if (warp == 1) tmem_free<false>(tmem, S::kColumns);
@@ -733,7 +756,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
     constexpr int kSums = GATED ? 2 : 1;
     extern __shared__ unsigned char raw[];
     __shared__ volatile int dead;
-    __shared__ volatile uint32_t filled;
+    __shared__ volatile uint32_t filled, failed;                  // failed: a block of the cluster gave up
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t barriers[2 * S::kMostStages + 2];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
@@ -744,7 +767,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         dead = 0;
-        filled = 0;
+        filled = failed = 0;
         for (uint32_t s = 0; s < stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1); mbar_init(flushed, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -764,13 +787,13 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
     const uint32_t chunks = (p.k + kBK - 1) / kBK;
     const uint32_t first = chunks * rank / SPLIT, last = chunks * (rank + 1) / SPLIT;       // at least one: SPLIT <= chunks
     const uint32_t stage_bytes = S::stage(p.a_rows), at_scales = S::kCodesB + p.a_rows * 128;     // scales of A, B and B's second matrix
+    const bool leader = elect();
+    uint32_t issued = 0;                                         // warp 0: fillings of stages
 
     if (warp == 0) {
-        const bool leader = elect();
-        uint32_t s = 0, round = 0, it = 0;
-        bool ok = true;
-        for (uint32_t c = first; c < last; ++c, ++it) {
-            if (!(ok = warp_wait(empty(s), (round & 1) ^ 1, &dead, &filled))) break;
+        uint32_t s = 0, round = 0;
+        for (uint32_t c = first; c < last; ++c, ++issued) {
+            if (!warp_wait(empty(s), (round & 1) ^ 1, &dead, &filled)) break;
             if (leader) {
                 const uint32_t at = base + s * stage_bytes, scales = at + at_scales;
                 const uint32_t bytes = (p.k + 127) / 128 - 2 * c < 2 ? 512 : 1024;
@@ -781,16 +804,12 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
                 if constexpr (GATED != 0) bulk_load(scales + 2048, p.b1_scales + (n0 / 128) * p.b1_band + c * 1024ull, bytes, full(s));
                 tma_load(at + S::kCodesB, &map_a, c * (kBK / 2), 0, full(s));
                 bulk_load(scales, p.a_scales + c * 1024ull, bytes, full(s));
-                filled = it + 1;
+                filled = issued + 1;
             }
             __syncwarp();
             if (++s == stages) { s = 0; ++round; }
         }
-        if (!ok && leader)                                       // nothing may still be on its way into a block that ends
-            for (uint32_t j = it > stages ? it - stages : 0; j < it; ++j) mbar_wait(full(j % stages), (j / stages) & 1);
-        __syncwarp();
     } else if (warp == 1) {
-        const bool leader = elect();
         const uint32_t last_steps = (p.k - (chunks - 1) * kBK + 63) / 64;
         uint32_t s = 0, round = 0;
         bool ok = true;
@@ -818,15 +837,19 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
             __syncwarp();
             if (++s == stages) { s = 0; ++round; }
         }
-        if (leader) {
-            if (ok) mma_commit<false>(done);
-            else {                                               // let the multiplications that were issued come to an end
-                mma_commit<false>(flushed);
-                mbar_wait(flushed, 0);
-            }
-        }
+        if (ok && leader) mma_commit<false>(done);
         __syncwarp();
     }
+    // Where a wait ran out: lets all that was issued end, before its memory is used again or the block leaves.
+    const auto settle = [&] {
+        if (dead == 0) return;
+        if (warp == 0 && leader) for_outstanding(issued, stages, [&](uint32_t s, uint32_t parity) { mbar_wait(full(s), parity); });
+        if (warp == 1 && leader) {
+            mma_commit<false>(flushed);
+            mbar_wait(flushed, 0);
+        }
+        __syncwarp();
+    };
     // Two warps for each quarter of the lanes, 32 columns or features: they take eight rows in turn.
     const uint32_t quarter = warp % 4, half = (warp - 2) / 4;
     const uint32_t from = tmem + ((quarter * 32) << 16);
@@ -869,7 +892,9 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
         // what a block receives: from each block, for each row, its slice of g (or C) and of u
         const auto place = [&](uint32_t b, uint32_t r, uint32_t w, uint32_t col) { return base + (((b * p.m + r) * kSums + w) * kSlice + col) * 4; };
         __syncthreads();
+        settle();
         cluster_sync();                                          // all blocks have multiplied: the stages are free
+        if (dead != 0 && threadIdx.x < SPLIT) tell_block(&failed, threadIdx.x, 1);
         if (warp >= 2 && fine) {
             const uint32_t col = quarter * 32 + lane, owner = col / kSlice;
 #pragma unroll 1
@@ -890,7 +915,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
         cluster_sync();
         if constexpr (GATED != 0) {
             constexpr uint32_t kBlocks = kSlice / 32;            // SPLIT is 2 or 4
-            for (uint32_t item = warp; item < p.m * kBlocks; item += kSplitThreads / 32) {
+            for (uint32_t item = warp; item < p.m * kBlocks && !failed; item += kSplitThreads / 32) {
                 const uint32_t r = item / kBlocks, j = item % kBlocks;
                 float g = 0.0f, u = 0.0f;
 #pragma unroll
@@ -898,7 +923,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
                 store_gated_warp<GATED == 2>(p, r, n0 + rank * kSlice + 32 * j, g, u);
             }
         } else {
-            for (uint32_t item = threadIdx.x; item < p.m * kSlice; item += kSplitThreads) {
+            for (uint32_t item = threadIdx.x; item < p.m * kSlice && !failed; item += kSplitThreads) {
                 const uint32_t r = item / kSlice, col = n0 + rank * kSlice + item % kSlice;
                 float x = 0.0f;
 #pragma unroll
@@ -910,6 +935,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) mx_token_kernel(const __grid
     __syncwarp();
     fence_before();
     __syncthreads();
+    if constexpr (SPLIT == 1) settle();
     if (threadIdx.x == 0 && dead) atomicAdd(&g_product_wait_expired, 1u);
     fence_after();
     if (warp == 1) tmem_free<false>(tmem, S::kColumns);
