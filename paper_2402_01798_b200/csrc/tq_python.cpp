@@ -9,6 +9,7 @@
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -695,6 +696,9 @@ PyObject* maker(PyObject*, PyObject* const* args, Py_ssize_t n) {
         Args a(args, n);
         return CALL(a);
     } catch (const Failed&) {
+        return nullptr;
+    } catch (const c10::OutOfMemoryError&) {           // as from torch.empty
+        torch::translate_exception_to_python(std::current_exception());
         return nullptr;
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());

@@ -1,4 +1,4 @@
-"""Calls as the binding takes them: sizes that do not fit, and the memory of what a call makes for a given stream."""
+"""Calls as the binding takes them: sizes that do not fit, memory that runs out, and the memory of what a call makes for a given stream."""
 import pytest
 import torch
 
@@ -60,6 +60,13 @@ def test_parts_of_larger_tensors_are_taken(tq):
     out = torch.full((104,), -7.0, device="cuda")
     tq.tq_mx_decompress_aggregate(rows, out=out)
     assert torch.equal(out[:96], tq.tq_mx_decompress_aggregate(rows)) and (out[96:] == -7).all()
+
+
+def test_memory_that_runs_out(tq):
+    """The error is torch's own for that, which programs catch to make room."""
+    for call in (lambda: tq.new_mx(2 ** 31 - 1, 2 ** 24), lambda: tq.tq_mx_product(*[tq.MxMatrix(None, None, 2 ** 21, 0, memory=ones(1).byte())] * 2, torch.float32)):
+        with pytest.raises(torch.OutOfMemoryError):
+            call()
 
 
 # ---- a stream given by hand: what the call makes is that stream's memory -------------------------------------------------
