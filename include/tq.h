@@ -404,7 +404,7 @@ size_t tq_mx_scale_stride(uint64_t cols, tq_mx_layout layout);
 /*
  * Quantisation of x [out->rows][out->cols] along its rows.
  *   x_dev        elements of `dtype`, aligned to their size; x_stride >= cols elements from row to row.  Rows that start on 16-byte
- *                boundaries are read fastest.
+ *                boundaries are read fastest, messages of a few long rows up to ten times as fast as on any other boundary.
  *   seed, first_row  stochastic rounding only.  Element (r, c) draws its 16 bits as in tq_compress: Philox4x32-10 with key = seed and
  *                counter = (c >> 3, first_row + r, 0), slot c & 7.  With p the place between its two neighbours on the grid it goes
  *                to the upper one when the bits are below rint(p * 2^16).

@@ -253,7 +253,8 @@ constexpr int kBK = 256;                                         // elements of 
 // Tensor memory: two accumulators of 256 columns that overlap in the middle, at 0 and 112, and the scales of 6 stages from 368 on.  The
 // columns that both use are taken out first, and the next tile begins when they are.  The scales have a place for each stage, so that no copy can
 // meet a multiplication that still reads them: a stage is only filled again when its multiplications are done.
-// 8192^3: 182 us, 6.0 PFLOP/s, the tensor pipe 73 % busy; after a second of it the 1 kW limit lowers the clock and it is 216.
+// 8192^3: 182 us, 6.0 PFLOP/s, the tensor pipe 75 % busy; after a second of it the 1 kW limit lowers the clock and it is 217.  Gated, 8192 tokens, 8192 x 8192, with the projections
+// kept: 70 %.
 constexpr int kPairStages = 6, kPairThreads = 320;
 constexpr uint32_t kPairCodes = 2 * 128 * kBK / 2, kPairStage = kPairCodes + 3 * 1024;       // A, B; scales of 128 rows of A and of 256 rows of B
 constexpr uint32_t kPairSmem = kPairStages * kPairStage + 1024 + 256;
@@ -261,8 +262,9 @@ constexpr uint32_t kSecond = 112, kPairScales = kSecond + 256, kPairScaleColumns
 static_assert(kPairScales + kPairStages * kPairScaleColumns == 512, "tensor memory has 512 columns");
 
 // Tile t of the result.  The tiles that are worked on at a time are a column of `group` tiles and as many to its right as there are clusters: where both operands fit
-// the L2 together the whole height is taken, else 4, so that a wave of tiles reads little of either (8192 x 4096 x 16384, 107 MB of operands: 202 us with the whole height,
-// 180 with 4, after a second of it 240 and 208; 8192^3, 71 MB: 188 and 192).
+// the L2 together the whole height is taken, else 4, so that a wave of tiles reads little of either.  Whole height / 4, us: 8192 x 4096 x 16384, 107 MB of operands, 202 / 180;
+// 16384 x 4096 x 8192, 89 MB, 237 / 213; 5400 x 5000 x 16384, 91 MB, 176 / 173; 8192^3, 71 MB, 183 / 188; 8192 x 8192 x 4096, 36 MB, 103 / 104; 4096 x 16384 x 8192, 8192 x 8192 x 10240
+// and gated blocks of 71 to 107 MB within 2 % of one another.  It loses where A alone fits: 8192 x 8192 x 12288, 107 MB, 290 / 316.
 struct PairTile {
     uint32_t m, n;
     __device__ __forceinline__ PairTile(const ProductArgs& p, uint32_t t) {
@@ -710,7 +712,10 @@ __global__ void __launch_bounds__(kSplitThreads, 1) mx_split_kernel(const __grid
 // 16 KB of B (1 x 8192 x 8192 read 2.5 TB/s).  Two blocks an SM, so that one loads while the other starts or ends.
 // A thread of the epilogue has one column of C, or feature, for all rows; 32 features of a row are a warp's, and so is their block of h.
 constexpr uint32_t kMostTokens = 64;
-constexpr uint32_t kMostGatedTokens = 16;                        // beyond, the activation of one row after another takes too long (64 x 2048 x 16384: 15 us, split blocks 7)
+// Beyond, the activation of one row after another takes too long.  This kernel / split blocks, us: 8 x 1024 x 2048 5.0 / 6.2, 16 6.3 / 6.2, 24 7.0 / 5.8, 64 12 / 5.6; 16 x 4096 x 8192
+// 8.1 / 10, 24 9.0 / 10, 32 10 / 10, 64 14 / 8.8; 16 x 2048 x 16384 8.9 / 9.6, 24 9.9 / 9.6, 64 16 / 8.9; 16 x 8192 x 8192 11 / 16, 32 13 / 11.  Without a gate: 48 x 1000 x 4000 4.8 / 5.5, 64 5.2 / 5.7;
+// 48 x 8192 x 4096 6.8 / 7.4, 64 7.5 / 6.6; 32 x 4096 x 8192 6.5 / 6.6, 64 8.0 / 7.0; 16 x 16384 x 2048 5.4 / 6.5, 64 7.6 / 5.9.
+constexpr uint32_t kMostGatedTokens = 16;
 template <int GATED>
 struct TokenShape {
     static constexpr uint32_t kCodesB = (GATED ? 256 : 128) * kBK / 2, kScaleBytes = (GATED ? 3 : 2) * 1024;
@@ -996,8 +1001,10 @@ constexpr size_t kMostSplitSmem = 212 * 1024, kMostTokenSmem = 109 * 1024;      
 
 // Which kernel, and how many blocks share a tile: by an estimate of the time in ns, fitted to graphs of 20 launches.  A pair takes 430 a stage and 1300 a
 // tile at least; a split block 310 (two B matrices: 365) and up to 70 more as the SMs fill.  Adding up costs 1 us and 4 ns for each row and block.
-// Measured (pair / split 1 / 2 / 4 / 8): 777 x 1000 x 4000 12.6 / 10.3 / 8.9 / 14 / 17 us, 1024 x 2048 x 4096 9.9 / 8.4 / 14 / 24 / 33, 2048^3 8.2 / 11 / 23 / 30 / 59,
-// 128 x 4096 x 4096 9.8 / 7.8 / 7.2 / 6.4 / 9.0, gated 512 x 4096 x 8192 17 / 19 / 36 / 71.
+// Measured (pair / split 1 / 2 / 4 / 8, us; a graph of 20): 65 x 1024 x 1024 5.4 / 3.6 / 4.5 / 4.3, 128 x 4096 x 4096 9.8 / 7.7 / 7.2 / 6.7 / 9.3, 128 x 16384 x 2048 8.5 / 5.8 / 12 / 16 / 32,
+// 128 x 4096 x 16384 24 / 22 / 15 / 11 / 22, 250 x 1024 x 4096 9.3 / 7.4 / 6.9 / 6.2 / 8.1, 777 x 1000 x 4000 10.4 / 8.6 / 7.7 / 13 / 17, 512 x 8192 x 2048 8.6 / 11 / 24 / 31 / 61,
+// 1024 x 2048 x 4096 10 / 8.5 / 15 / 26 / 35, 2048 x 2048 x 512 6.6 / 7.6 / 14, 2048^3 8.6 / 11 / 24 / 31 / 61, gated 65 x 4096 x 8192 11 / 9.6 / 8.9 / 17, gated 512 x 4096 x 8192 18 / 20 / 38 / 73.
+// Of 35 such shapes it takes the fastest, or one within 5 %, in 33; eight blocks would be better for 256 x 256 x 8192 (7.2, 6.2) and 300 x 300 x 8192 (7.7, 6.8).
 struct ProductPlan {
     bool pair;
     uint32_t split;

@@ -162,7 +162,10 @@ __device__ __forceinline__ int within(uint64_t size, uint64_t from, int most) {
     return from >= size ? 0 : size - from < static_cast<uint64_t>(most) ? static_cast<int>(size - from) : most;
 }
 
-// 8192 x 4096 bf16 along both axes: nearest 23.5 us (4.4 TB/s), stochastic 44, the integer and fma-heavy pipes 60 % busy each with 32 instructions an element.
+// 8192 x 4096 bf16 along both axes: nearest 23.5 us (4.4 TB/s), where warps wait for memory and the shared-memory pipe is 67 % busy; stochastic 44, 32 instructions an
+// element: 72 % of the issue slots, the integer and fma-heavy pipes 60 % each, none of them full; warps wait for a pipe or to be dispatched, hardly for memory.
+// Rows on any boundary: 8191 x 5003 fp32 along rows 32 us nearest, 52 stochastic, bf16 50 and 85.  A tile is 64 rows high whether there are so many or not: 16 messages of 25.6 M
+// fp32 that follow one another without padding take 3.2 ms, on 16-byte boundaries 0.32.
 template <bool BF16, bool STOCHASTIC, bool BOTH>
 __global__ void __launch_bounds__(kThreads, 4) mx_tile_kernel(MxInput in, MxView out, MxView out_t, uint32_t tiles_across, RoundKeys keys, uint32_t first_row) {
     extern __shared__ __align__(16) unsigned char raw[];
@@ -508,8 +511,9 @@ __device__ __forceinline__ void take_ahead(const MxAhead& a, int j, const MxItem
     }
 }
 
-// A block takes tile after tile.  AHEAD: as above, 102 KB of shared memory, two blocks an SM.  8192 x 8192 bf16: stochastic 250 us, 93 instructions a feature at 0.7 a
-// clock and scheduler; nearest 154 (3.8 TB/s).  Three blocks a tile, one for each of dg, du and h, with half the registers: 331.
+// A block takes tile after tile.  AHEAD: as above, 102 KB of shared memory, two blocks an SM.  8192 x 8192 bf16: stochastic 286 us, 106 instructions a feature at 0.7 a
+// clock and scheduler; nearest 183 (3.2 TB/s), 67 instructions; GELU 313 and 204.  (With an exponential that is flushed below 2^-126 250 and 154, but gates below -87 came out as zeros.)
+// Three blocks a tile, one for each of dg, du and h, with half the registers, took 331 where this took 274.
 template <bool BF16, bool AHEAD, bool GELU, bool STOCHASTIC>
 __global__ void __launch_bounds__(kThreads, 2) mx_gated_backward_kernel(MxGatedInput in, MxView dgu, MxView dgu_t, MxView h_t, uint32_t tiles_across, uint32_t tiles, RoundKeys keys) {
     extern __shared__ __align__(16) unsigned char raw[];
