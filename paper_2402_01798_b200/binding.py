@@ -186,6 +186,8 @@ def _empty(size, dtype: torch.dtype, device, stream) -> torch.Tensor:
     if device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
     handle, current = int(getattr(stream, "cuda_stream", stream)), torch.cuda.current_stream(device)
+    if handle == 1:                                # cudaStreamLegacy, which torch knows as 0
+        handle = 0
     if handle == current.cuda_stream:
         return torch.empty(size, dtype=dtype, device=device)
     with torch.cuda.stream(torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)):

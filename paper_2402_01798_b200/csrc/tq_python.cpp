@@ -494,7 +494,8 @@ at::Tensor empty_like_device(const at::Tensor& like, at::IntArrayRef sizes, at::
     const auto make = [&] { return at::detail::empty_generic(sizes, c10::GetAllocator(c10::kCUDA), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt); };
     if (stream == Py_None) return make();
     const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream();
-    const cudaStream_t given = static_cast<cudaStream_t>(Args::stream_of(stream));
+    cudaStream_t given = static_cast<cudaStream_t>(Args::stream_of(stream));
+    if (given == cudaStreamLegacy) given = nullptr;                // two names of one stream; torch knows the other
     if (current.stream() == given) return make();
     const c10::cuda::CUDAStreamGuard on(c10::cuda::getStreamFromExternal(given, like.device().index()));
     at::Tensor t = make();

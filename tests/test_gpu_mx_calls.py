@@ -140,6 +140,22 @@ def test_results_are_memory_of_the_given_stream(tq):
             assert all(pool_of(t) == current.cuda_stream for t in got), name
 
 
+def test_handles_of_the_default_streams(tq):
+    """0 and 1 are the legacy default stream, 2 is the thread's own: CUDA's names for them, taken by every call and from every current stream."""
+    for name, call in calls(tq).items():
+        want = [t.clone() for t in tensors(call(None))]
+        torch.cuda.synchronize()
+        for current in (torch.cuda.default_stream(), torch.cuda.Stream()):
+            with torch.cuda.stream(current):
+                for handle in (0, 1, 2):
+                    got = tensors(call(handle))
+                    torch.cuda.synchronize()
+                    for t, w in zip(got, want, strict=True):
+                        assert pool_of(t) == (2 if handle == 2 else 0), (name, handle)
+                        if not name.startswith("mx"):
+                            assert torch.equal(t, w), (name, handle)
+
+
 def test_memory_in_use_on_the_current_stream_is_left_alone(tq):
     """A block that the current stream frees while a slow kernel there has yet to read it: a call on another stream takes none of it."""
     m = tq.tq_mx_quantize(torch.randn(1024, 1024, device="cuda"))
